@@ -176,6 +176,37 @@ GKV_API int gkv_decode_attn(gkv_cache* c, int32_t layer, const void* q, const in
 GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, float* out, float* lse,
                                     float* block_mass, float* certificate, void* stream);
 
+/* ---- the prompt: attention and token masses before the ingest ----
+ * Packed sequences of one layer: sequence s has the rows [offsets[s], offsets[s + 1]) of every buffer; a sequence may be
+ * empty.  Rows that no sequence has are neither read for a result nor written.  Zero-initialise, then set struct_size and
+ * abi_version.  Grouped-query layout with head dim 128 and up to 8 query heads per KV head (GKV_ERR_UNSUPPORTED else).
+ * The buffers must lie on the current device (GKV_ERR_INVALID_ARG else), and results must not overlap inputs. */
+typedef struct gkv_prompt {
+  uint32_t struct_size;   /* sizeof(gkv_prompt) */
+  uint32_t abi_version;   /* GKV_ABI_VERSION */
+  int32_t n_seqs, n_q_heads, n_kv_heads, head_dim;
+  const int32_t* offsets; /* HOST int32 [n_seqs + 1], ascending from >= 0; read during the call only */
+  int64_t q_stride, k_stride, v_stride, out_stride; /* elements from one row to the next, a multiple of 8; 0 = heads * head_dim.
+                                                       (A row's heads follow one another: rows may be slices of a fused projection.) */
+  float softmax_scale;    /* 0 -> 1/sqrt(head_dim) */
+} gkv_prompt;
+
+/* Causal attention of every query head over the exact rows of its own sequence (Sec. 3.1, Eq. 1 before anything is demoted):
+ * query row i attends to rows 0 .. i of its sequence.  No workspace; the call is asynchronous and may be captured into a graph.
+ *   q    device bf16 [rows][n_q_heads][128]      k, v  device bf16 [rows][n_kv_heads][128]      (16-byte aligned)
+ *   out  device bf16 [rows][n_q_heads][128], 16-byte aligned (rounded once, from fp32 accumulators; weights enter the
+ *        value product as bf16)
+ *   lse  device fp32 [rows][n_q_heads], packed, natural-log sum of exp(logit), or NULL */
+GKV_API int gkv_prompt_attn(const gkv_prompt* p, const void* q, const void* k, const void* v, void* out, float* lse, void* stream);
+
+/* Attention mass of every prompt token (Sec. 3.1, Eq. 2): the softmax weight that the newest min(n_obs, length) queries of its
+ * sequence give it, averaged over them and over the query heads of the KV head; a sequence's masses of one KV head sum to 1.
+ *   q, k  as for gkv_prompt_attn (v_stride and out_stride are not used)
+ *   lse   device fp32 [rows][n_q_heads] of gkv_prompt_attn; the observing rows are read
+ *   mass  device fp32, sequence after sequence from offsets[0] on, [n_kv_heads][length] each: for sequences of one length this
+ *         is the token_mass [batch][n_kv_heads][n_new] of gkv_append_demote */
+GKV_API int gkv_prompt_mass(const gkv_prompt* p, const void* q, const void* k, const float* lse, int32_t n_obs, float* mass, void* stream);
+
 /* Per-block bounds behind the certificate (parity checks; synchronises the device).
  *   bounds_out  HOST fp32 [batch][n_kv_heads][n_closed][4]: kappa_b, delta_b, max_j |v_j|, 0 */
 GKV_API int gkv_debug_export_bounds(gkv_cache* c, int32_t layer, float* bounds_out);

@@ -30,6 +30,7 @@ EXPORTS = [
     "gkv_debug_replan_levels",
     "gkv_quest_select", "gkv_quest_select_static", "gkv_debug_export_boxes", "gkv_debug_export_scores", "gkv_bits_report",
     "gkv_debug_export_block", "gkv_debug_export_residual", "gkv_debug_export_units",
+    "gkv_prompt_attn", "gkv_prompt_mass",
     "gkv_debug_export_levels", "gkv_debug_plan_levels", "gkv_ctx_len", "gkv_strerror", "gkv_last_cuda_error",
 ]
 
@@ -53,6 +54,16 @@ class GkvBits(C.Structure):
         ("residual_index_bits", C.c_uint64), ("box_bits", C.c_uint64), ("resident_bits", C.c_uint64),
         ("meta_bits", C.c_uint64), ("last_read_bits", C.c_uint64), ("blocks_by_level", C.c_uint64 * 5),
         ("bpv_resident", C.c_double), ("bpv_paper", C.c_double), ("bpv_read", C.c_double),
+    ]
+
+
+class GkvPrompt(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("abi_version", C.c_uint32),
+        ("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("offsets", C.c_void_p),
+        ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("out_stride", C.c_int64),
+        ("softmax_scale", C.c_float),
     ]
 
 
@@ -97,6 +108,8 @@ def load():
     lib.gkv_debug_export_boxes.argtypes = [vp, i32, i32, i32, vp, vp, i32, C.POINTER(i32)]
     lib.gkv_debug_export_scores.argtypes = [vp, i32, vp, vp, vp]
     lib.gkv_quest_select_static.argtypes = [vp, i32, vp, i32, vp, C.POINTER(i32), vp]
+    lib.gkv_prompt_attn.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, vp, vp, vp]
+    lib.gkv_prompt_mass.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, i32, vp, vp]
     lib.gkv_bits_report.argtypes = [vp, i32, C.POINTER(GkvBits)]
     lib.gkv_debug_export_block.argtypes = [vp, i32, i32, i32, i32, i32, C.POINTER(i32), vp, vp, vp, vp, C.POINTER(i32)]
     lib.gkv_debug_export_residual.argtypes = [vp, i32, i32, i32, vp, i32, C.POINTER(i32)]
@@ -206,6 +219,77 @@ def gkv_debug_replan_levels(cfg: GkvConfig, n_tail: int, mass, rng, prev):
                                           pv.ctypes.data_as(bp), levels.ctypes.data_as(bp), C.byref(miss)),
            "gkv_debug_replan_levels")
     return levels, bool(miss.value)
+
+
+def _rows(t, name, dtype, shape=None):
+    """A tensor [rows][heads][128] whose heads follow one another; returns the distance of its rows."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or t.dim() != 3 or t.shape[2] != 128:
+        raise ValueError(f"{name}: a CUDA {dtype} tensor [rows][heads][128] is needed")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != 128)):
+        raise ValueError(f"{name}: the heads of a row have to follow one another")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * 128
+
+
+def _floats(t, name, n, shape=None):
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or t.numel() < n or (
+            shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: a contiguous CUDA float32 tensor {list(shape) if shape is not None else [n]} is needed")
+
+
+def _prompt(q, k, offsets, softmax_scale, *more):
+    off = np.ascontiguousarray(offsets, dtype=np.int32)
+    if off.ndim != 1 or off.size < 1:
+        raise ValueError("offsets: n_seqs + 1 row numbers are needed")
+    if off[-1] > q.shape[0]:
+        raise ValueError(f"offsets: end at row {off[-1]} of {q.shape[0]}")
+    if any(t is not None and t.device != q.device for t in (k, *more)):
+        raise ValueError("all tensors have to be on one device")
+    d = GkvPrompt()
+    d.struct_size, d.abi_version = C.sizeof(GkvPrompt), GKV_ABI_VERSION
+    d.n_seqs, d.n_q_heads, d.n_kv_heads, d.head_dim = off.size - 1, q.shape[1], k.shape[1], q.shape[2]
+    d.offsets, d.softmax_scale = off.ctypes.data, softmax_scale
+    return d, off
+
+
+def _on(device, call):
+    """call(stream) with `device` current, on its current stream."""
+    if device.index == torch._C._cuda_getDevice():
+        return call(_stream())
+    with torch.cuda.device(device):
+        return call(_stream())
+
+
+def gkv_prompt_attn(q, k, v, out, offsets, lse=None, softmax_scale=0.0):
+    """Causal attention of packed prompts: q, out cuda bf16 [rows][n_q_heads][128], k, v cuda bf16 [rows][n_kv_heads][128]
+    (rows may be slices of a fused projection), offsets: host row numbers, sequence s = rows [offsets[s], offsets[s + 1]);
+    lse: cuda fp32 [rows][n_q_heads] or None.  Rows of no sequence are left as they are."""
+    qs, ks = _rows(q, "q", torch.bfloat16), _rows(k, "k", torch.bfloat16)
+    vs, os_ = _rows(v, "v", torch.bfloat16, k.shape), _rows(out, "out", torch.bfloat16, q.shape)
+    if k.shape[0] != q.shape[0]:
+        raise ValueError(f"k: {k.shape[0]} rows, not {q.shape[0]}")
+    if lse is not None:
+        _floats(lse, "lse", 0, q.shape[:2])
+    d, _keep = _prompt(q, k, offsets, softmax_scale, v, out, lse)
+    d.q_stride, d.k_stride, d.v_stride, d.out_stride = qs, ks, vs, os_
+    rc = _on(q.device, lambda st: load().gkv_prompt_attn(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), st))
+    return rc if rc == OK else _check(rc, "gkv_prompt_attn")
+
+
+def gkv_prompt_mass(q, k, lse, mass, offsets, n_obs, softmax_scale=0.0):
+    """Attention masses of prompt tokens under the newest n_obs queries of their sequence: q, k, offsets as for
+    gkv_prompt_attn, lse the log-sum-exp that it wrote; mass: cuda fp32, [n_kv_heads][length] sequence after sequence (for
+    sequences of one length the token_mass that gkv_append_demote takes)."""
+    qs, ks = _rows(q, "q", torch.bfloat16), _rows(k, "k", torch.bfloat16)
+    if k.shape[0] != q.shape[0]:
+        raise ValueError(f"k: {k.shape[0]} rows, not {q.shape[0]}")
+    _floats(lse, "lse", 0, q.shape[:2])
+    d, off = _prompt(q, k, offsets, softmax_scale, lse, mass)
+    _floats(mass, "mass", int(off[-1] - off[0]) * k.shape[1])
+    d.q_stride, d.k_stride = qs, ks
+    rc = _on(q.device, lambda st: load().gkv_prompt_mass(C.byref(d), _ptr(q), _ptr(k), _ptr(lse), n_obs, _ptr(mass), st))
+    return rc if rc == OK else _check(rc, "gkv_prompt_mass")
 
 
 class Cache:
