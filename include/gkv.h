@@ -176,6 +176,27 @@ GKV_API int gkv_decode_attn(gkv_cache* c, int32_t layer, const void* q, const in
 GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, float* out, float* lse,
                                     float* block_mass, float* certificate, void* stream);
 
+/* Attention of n_new new tokens per sequence over the graded cache of `layer` and, causally, over one another (the multi-query
+ * form of Sec. 3.7): verification of drafted tokens, or the next turn of a conversation.  Query token i of a sequence attends to
+ * everything the cache holds, as gkv_decode_attn reads it, and to the chunk's own exact rows 0 .. i.  The cache is not changed: rows that
+ * are to stay are appended with gkv_append_demote afterwards.  It may be empty.  Grouped-query layout only (GKV_ERR_UNSUPPORTED with v_aliases_k).
+ *   q      device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned
+ *   k_new, v_new  device bf16 [batch][n_new][n_kv_heads][128], 16-byte aligned
+ *   len    HOST int32 [batch], 0 .. n_new: real tokens of each sequence (the rest of its rows is neither read for a result nor
+ *          written), read during the call only; or NULL = n_new everywhere.  At most 1024 sequences with lengths (GKV_ERR_UNSUPPORTED)
+ *   out    device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned: rounded once from fp32 accumulators; weights enter the
+ *          value product with 8 (exact rows) or 11 (quantised blocks) bits, quantised keys and values with 11
+ *   lse    device fp32 [batch][n_new][n_q_heads], natural-log sum of exp(logit), or NULL
+ *   workspace  device, 16-byte aligned, gkv_chunk_workspace_bytes long: partial results of the call, free again when its kernels
+ *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too)
+ * All buffers and the arena must lie on the current device (GKV_ERR_INVALID_ARG else).  The bits that the call reads are not counted by gkv_bits_report.
+ * A captured call replays the context length of its capture: capture again after an append. */
+GKV_API int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that are enough for every gkv_chunk_attn of n_new tokens (below 20 MB).  bytes: host out. */
+GKV_API int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t n_new, size_t* bytes);
+
 /* ---- the prompt: attention and token masses before the ingest ----
  * Packed sequences of one layer: sequence s has the rows [offsets[s], offsets[s + 1]) of every buffer; a sequence may be
  * empty.  Rows that no sequence has are neither read for a result nor written.  Zero-initialise, then set struct_size and

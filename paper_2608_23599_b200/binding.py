@@ -30,7 +30,7 @@ EXPORTS = [
     "gkv_debug_replan_levels",
     "gkv_quest_select", "gkv_quest_select_static", "gkv_debug_export_boxes", "gkv_debug_export_scores", "gkv_bits_report",
     "gkv_debug_export_block", "gkv_debug_export_residual", "gkv_debug_export_units",
-    "gkv_prompt_attn", "gkv_prompt_mass",
+    "gkv_prompt_attn", "gkv_prompt_mass", "gkv_chunk_attn", "gkv_chunk_workspace_bytes",
     "gkv_debug_export_levels", "gkv_debug_plan_levels", "gkv_ctx_len", "gkv_strerror", "gkv_last_cuda_error",
 ]
 
@@ -108,6 +108,8 @@ def load():
     lib.gkv_debug_export_boxes.argtypes = [vp, i32, i32, i32, vp, vp, i32, C.POINTER(i32)]
     lib.gkv_debug_export_scores.argtypes = [vp, i32, vp, vp, vp]
     lib.gkv_quest_select_static.argtypes = [vp, i32, vp, i32, vp, C.POINTER(i32), vp]
+    lib.gkv_chunk_attn.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.gkv_chunk_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
     lib.gkv_prompt_attn.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, vp, vp, vp]
     lib.gkv_prompt_mass.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, i32, vp, vp]
     lib.gkv_bits_report.argtypes = [vp, i32, C.POINTER(GkvBits)]
@@ -355,6 +357,48 @@ class Cache:
             rc = load().gkv_decode_attn_observe(self.handle, layer, _ptr(q), _ptr(out), _ptr(lse), _ptr(block_mass),
                                                 _ptr(certificate), self._st())
         return rc if rc == OK else _check(rc, "gkv_decode_attn_observe")
+
+    def gkv_chunk_workspace_bytes(self, n_new) -> int:
+        n = C.c_size_t(0)
+        _check(load().gkv_chunk_workspace_bytes(self.handle, n_new, C.byref(n)), "gkv_chunk_workspace_bytes")
+        return n.value
+
+    def gkv_chunk_attn(self, layer, q, k_new, v_new, out, lse=None, lengths=None, workspace=None):
+        """Attention of n_new new tokens per sequence over the cache and, causally, over one another; the cache stays as it is.
+        q, out: cuda bf16 [B][n_new][Hq][128]; k_new, v_new: cuda bf16 [B][n_new][Hkv][128]; lse: cuda fp32 [B][n_new][Hq] or
+        None; lengths: host ints [B] (rows from there on are left as they are) or None; workspace: a cuda tensor of
+        gkv_chunk_workspace_bytes bytes, or None (one is taken from torch's allocator for the call)."""
+        b, hq, hkv, dev = self.cfg.batch, self.cfg.n_q_heads, self.cfg.n_kv_heads, self.arena.device
+        n = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 4 else 0
+        for t, name, h, dt in ((q, "q", hq, torch.bfloat16), (k_new, "k_new", hkv, torch.bfloat16), (v_new, "v_new", hkv, torch.bfloat16),
+                               (out, "out", hq, torch.bfloat16), (lse, "lse", hq, torch.float32)):
+            if t is None and name == "lse":
+                continue
+            shape = (b, n, h) if name == "lse" else (b, n, h, 128)
+            if not isinstance(t, torch.Tensor) or tuple(t.shape) != shape or t.dtype != dt or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {dev} is needed")
+        ln = None
+        if lengths is not None:
+            ln = np.ascontiguousarray(lengths, dtype=np.int32)
+            if ln.shape != (b,):
+                raise ValueError(f"lengths: {b} of them are needed")
+
+        if workspace is not None and (not isinstance(workspace, torch.Tensor) or workspace.device != dev or not workspace.is_contiguous()):
+            raise ValueError(f"workspace: a contiguous tensor on {dev} is needed")
+
+        def call(st):
+            ws = workspace
+            if self.stream_handle is not None and self.stream_handle != st:
+                st = self.stream_handle
+                if ws is None:      # memory that is free again in the order of the stream that uses it
+                    with torch.cuda.stream(torch.cuda.ExternalStream(st, device=dev)):
+                        ws = torch.empty(self.gkv_chunk_workspace_bytes(n), dtype=torch.uint8, device=dev)
+            if ws is None:
+                ws = torch.empty(self.gkv_chunk_workspace_bytes(n), dtype=torch.uint8, device=dev)
+            return load().gkv_chunk_attn(self.handle, layer, _ptr(q), _ptr(k_new), _ptr(v_new), n, None if ln is None else ln.ctypes.data,
+                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), st)
+        rc = _on(dev, call)
+        return rc if rc == OK else _check(rc, "gkv_chunk_attn")
 
     def gkv_debug_export_bounds(self, layer):
         """Per-block certificate bounds as numpy [batch][n_kv_heads][n_closed][4] (kappa, delta, max |v|, 0)."""

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "../../include/gkv.h"
+#include "gkv_chunk.h"
 #include "gkv_internal.h"
 #include "gkv_mla.h"
 
@@ -1954,6 +1955,69 @@ int gkv_decode_attn(gkv_cache* c, int32_t layer, const void* q, const int32_t* p
 int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, float* out, float* lse, float* block_mass,
                             float* certificate, void* stream) {
   return decode_impl(c, layer, q, nullptr, 0, out, lse, true, block_mass, certificate, stream);
+}
+
+namespace {
+ChunkShape chunk_of(const gkv_cache* c, int32_t n_new) {
+  ChunkShape s{};
+  s.batch = c->cfg.batch;
+  s.n_kv_heads = c->cfg.n_kv_heads;
+  s.group = c->group;
+  s.n_new = n_new;
+  chunk_shape(&s);
+  return s;
+}
+}  // namespace
+
+int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t n_new, size_t* bytes) {
+  if (!c || !bytes || n_new <= 0) return GKV_ERR_INVALID_ARG;
+  if (is_mla(c->cfg)) return GKV_ERR_UNSUPPORTED;
+  const ChunkShape s = chunk_of(c, n_new);
+  // a cut adds a slot; without copies a CTA has at most two
+  const int64_t tiles = static_cast<int64_t>(c->n_streams) * s.row_tiles;
+  *bytes = static_cast<size_t>(std::min<int64_t>(kChunkParts, tiles + kChunkCtas - 1)) * kChunkSlotFloats * sizeof(float);
+  return GKV_OK;
+}
+
+int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len, void* out,
+                   float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0) return GKV_ERR_INVALID_ARG;
+  if (is_mla(c->cfg)) return GKV_ERR_UNSUPPORTED;
+  if (!q || !k_new || !v_new || !out) return GKV_ERR_INVALID_ARG;
+  if (misaligned(q, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(out, 16) || misaligned(lse, 4) || misaligned(workspace, 16))
+    return GKV_ERR_INVALID_ARG;
+  if (len) {
+    if (c->cfg.batch > kChunkMaxBatch) return GKV_ERR_UNSUPPORTED;
+    for (int b = 0; b < c->cfg.batch; ++b)
+      if (len[b] < 0 || len[b] > n_new) return GKV_ERR_INVALID_ARG;
+  }
+  if (!on_current_device({c->arena, q, k_new, v_new, out, lse, workspace})) return GKV_ERR_INVALID_ARG;
+  const LayerState& L = c->layers[layer];
+  ChunkCall call{};
+  call.shape = chunk_of(c, n_new);
+  call.shape.n_closed = L.n_closed;
+  call.shape.n_tail = L.n_tail;
+  if (L.has_residual)
+    for (int s = 0; s < c->n_streams; ++s) call.shape.res_groups = std::max(call.shape.res_groups, (L.res_count_h[s] + kChunkKeys - 1) / kChunkKeys);
+  ChunkCuts cuts;
+  ChunkMerge merge;
+  const int slots = chunk_plan(call.shape, len, &cuts, &merge);
+  if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
+  call.arena = c->arena;
+  call.table = L.table_d;
+  call.table_stride = c->table_stride;
+  call.res_off256 = L.res_off_d;
+  call.res_count = L.res_count_d;
+  call.q = static_cast<const uint16_t*>(q);
+  call.k_new = static_cast<const uint16_t*>(k_new);
+  call.v_new = static_cast<const uint16_t*>(v_new);
+  call.out = static_cast<uint16_t*>(out);
+  call.lse = lse;
+  call.workspace = static_cast<float*>(workspace);
+  call.status = c->status_d;
+  call.scale = c->scale;
+  CK(c, launch_chunk(call, cuts, merge, len, static_cast<cudaStream_t>(stream)));
+  return GKV_OK;
 }
 
 int gkv_debug_export_bounds(gkv_cache* c, int32_t layer, float* bounds_out) {

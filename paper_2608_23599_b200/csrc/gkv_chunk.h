@@ -1,0 +1,137 @@
+// The work of a chunk call (attention of several new tokens per sequence over the graded cache) and how it is cut into CTAs.
+// Host code without CUDA calls: it runs on a host alone as well.
+//
+// A tile is up to 128 rows of one stream: the query heads of `tile_tokens` consecutive new tokens.  It walks the stream's items: every
+// closed block, the partial block, the groups of 64 exact residual rows, and the chunk's own rows in groups of 64 as far as the tile's
+// last token sees them.  All tiles' items are laid end to end and cut into equal ranges, one per CTA, so a CTA has the end of one
+// tile, whole tiles, and the beginning of another.  A tile that was cut leaves partial results in slots; the slots of a tile follow one another.
+#pragma once
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace gkv {
+
+constexpr int kChunkRows = 128;            // rows of a tile
+constexpr int kChunkKeys = 64;             // keys of a step
+constexpr int kChunkCtas = 148;            // one CTA per SM: all of its tensor memory, most of its shared memory
+constexpr int kChunkMinItems = 4;          // items that a CTA is worth starting for
+constexpr int kChunkParts = 2 * kChunkCtas;      // most slots of a call, and most tiles to be merged
+constexpr int kChunkSlotFloats = kChunkRows * (128 + 2);
+
+constexpr int kChunkMaxBatch = 1024;       // sequences of a call with lengths of their own
+
+struct ChunkShape {
+  int32_t batch, n_kv_heads, group, n_new;
+  int32_t n_closed, n_tail, res_groups;      // residual groups: of the stream that has most
+  int32_t tile_tokens, row_tiles, copies;    // copies: see chunk_shape
+};
+
+inline int chunk_len(const ChunkShape& s, const int32_t* len, int b) { return len ? len[b] : s.n_new; }
+// items of row tile rt of a sequence with `len` new tokens
+#if defined(__CUDACC__)
+__host__ __device__
+#endif
+inline int chunk_items(const ChunkShape& s, int len, int rt) {
+  if (rt * s.tile_tokens >= len) return 0;
+  const int seen = (rt + 1) * s.tile_tokens < len ? (rt + 1) * s.tile_tokens : len;
+  return s.n_closed + (s.n_tail > 0) + s.res_groups + (seen + kChunkKeys - 1) / kChunkKeys;
+}
+
+// Tile size.  Where all rows of a stream fill at most half or a quarter of a tile, the tile holds them two or four times, and each copy takes
+// its share of a step's keys: the softmax of few rows is then spread over all warps.  Copies are merged with the slots, which
+// every tile then needs, so this is done up to as many streams as CTAs.
+inline void chunk_shape(ChunkShape* s) {
+  s->tile_tokens = kChunkRows / s->group;
+  s->copies = 1;
+  const int rows = s->n_new * s->group;
+  if (s->batch * s->n_kv_heads <= kChunkCtas && rows <= kChunkRows / 2) {
+    s->copies = rows <= kChunkRows / 4 ? 4 : 2;
+    s->tile_tokens = kChunkRows / s->copies / s->group;
+  }
+  s->row_tiles = (s->n_new + s->tile_tokens - 1) / s->tile_tokens;
+}
+
+struct ChunkCuts {
+  int32_t n;                                 // CTAs
+  int32_t tile[kChunkCtas + 1], item[kChunkCtas + 1];      // CTA c: from (tile, item) c to c + 1
+  int32_t slot[kChunkCtas];                  // its first slot
+};
+struct ChunkMerge {
+  int32_t n;                                 // tiles that left slots
+  int32_t tile[kChunkParts], slot[kChunkParts + 1];
+};
+
+// Does the part [begin, end) of a tile with `items` items go through a slot?
+#if defined(__CUDACC__)
+__host__ __device__
+#endif
+inline bool chunk_needs_slot(const ChunkShape& s, int begin, int end, int items) { return s.copies > 1 || begin > 0 || end < items; }
+
+// Returns the number of slots, or 0 with cuts->n = 0 where there is nothing to do.
+inline int chunk_plan(const ChunkShape& s, const int32_t* len, ChunkCuts* cuts, ChunkMerge* merge) {
+  int64_t total = 0;
+  for (int b = 0; b < s.batch; ++b) {
+    const int n = chunk_len(s, len, b);
+    for (int rt = 0; rt < s.row_tiles && rt * s.tile_tokens < n; ++rt) total += static_cast<int64_t>(s.n_kv_heads) * chunk_items(s, n, rt);
+  }
+  cuts->n = 0;
+  merge->n = 0;
+  merge->slot[0] = 0;
+  if (total == 0) return 0;
+  const int n_ctas = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / kChunkMinItems)));
+  // tiles in the order (sequence, KV head, row tile)
+  int64_t at = 0;
+  int c = 0, slots = 0, tile = 0;
+  for (int b = 0; b < s.batch; ++b) {
+    const int n = chunk_len(s, len, b);
+    for (int h = 0; h < s.n_kv_heads; ++h)
+      for (int rt = 0; rt < s.row_tiles; ++rt, ++tile) {
+        const int items = chunk_items(s, n, rt);
+        if (items == 0) continue;
+        int begin = 0;
+        const int first = slots;
+        while (begin < items) {
+          while (c < n_ctas && at + begin >= total * c / n_ctas) {      // CTA c begins here
+            cuts->tile[c] = tile;
+            cuts->item[c] = begin;
+            cuts->slot[c] = slots;
+            ++c;
+          }
+          const int64_t next = c < n_ctas ? total * c / n_ctas : total;
+          const int end = static_cast<int>(std::min<int64_t>(items, next - at));
+          if (chunk_needs_slot(s, begin, end, items)) ++slots;
+          begin = end;
+        }
+        at += items;
+        if (slots > first) {
+          merge->tile[merge->n++] = tile;
+          merge->slot[merge->n] = slots;
+        }
+      }
+  }
+  cuts->n = n_ctas;
+  cuts->tile[n_ctas] = s.batch * s.n_kv_heads * s.row_tiles;
+  cuts->item[n_ctas] = 0;
+  return slots;
+}
+
+#if defined(__CUDACC__)
+struct TableEntry;
+struct ChunkCall {
+  const uint8_t* arena;
+  const TableEntry* table;
+  const uint32_t* res_off256;
+  const int32_t* res_count;
+  const uint16_t *q, *k_new, *v_new;
+  uint16_t* out;
+  float *lse, *workspace;
+  uint32_t* status;
+  int32_t table_stride;
+  float scale;
+  ChunkShape shape;
+};
+cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
+#endif
+
+}  // namespace gkv

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "gkv_layout.cuh"
 
@@ -202,6 +203,8 @@ cudaError_t raise_smem_limit(void (*kernel)(Args...), size_t bytes, std::atomic<
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
 }
+
+bool on_current_device(std::initializer_list<const void*> ptrs);      // null pointers aside
 
 constexpr uint32_t kStatusRange = 1u;      // a scale or zero saturated
 constexpr uint32_t kStatusInternal = 2u;   // an index check failed inside a kernel

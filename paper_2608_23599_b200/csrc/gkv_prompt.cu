@@ -533,22 +533,6 @@ int check_prompt(const gkv_prompt* d, int* rows) {
   return GKV_OK;
 }
 
-// Device memory of the current device (or memory that every device reaches): the kernels must not be given another GPU's.
-bool here(std::initializer_list<const void*> ptrs) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  for (const void* p : ptrs) {
-    if (!p) continue;
-    cudaPointerAttributes a{};
-    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-      cudaGetLastError();
-      return false;
-    }
-    if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != dev)) return false;
-  }
-  return true;
-}
-
 // Sequences [begin, end) with rows, longest first, `per` tokens to a work item.
 template <int N>
 int deal(Seqs<N>& s, const int32_t* offsets, const std::vector<int>& order, int begin, int end, int per) {
@@ -598,6 +582,22 @@ float scale_of(const gkv_prompt* d) { return (d->softmax_scale > 0.f ? d->softma
 
 }  // namespace
 
+// Device memory of the current device (or memory that every device reaches): the kernels must not be given another GPU's.
+bool on_current_device(std::initializer_list<const void*> ptrs) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  for (const void* p : ptrs) {
+    if (!p) continue;
+    cudaPointerAttributes a{};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+      cudaGetLastError();
+      return false;
+    }
+    if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != dev)) return false;
+  }
+  return true;
+}
+
 // A map of [rows][heads][128] 16-bit elements: boxes of 64 channels x `heads_box` heads x `rows_box` rows, 128-byte swizzle.
 // Rows are `stride` elements apart.
 bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int heads, int64_t stride, int heads_box, int rows_box) {
@@ -627,7 +627,7 @@ int gkv_prompt_attn(const gkv_prompt* d, const void* q, const void* k, const voi
   const std::vector<int> order = longest_first(d);
   if (order.empty()) return GKV_OK;
   if (!q || !k || !v || !out || misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16) || misaligned(lse, 4)) return GKV_ERR_INVALID_ARG;
-  if (!here({q, k, v, out, lse})) return GKV_ERR_INVALID_ARG;
+  if (!on_current_device({q, k, v, out, lse})) return GKV_ERR_INVALID_ARG;
   const int64_t nq = static_cast<int64_t>(d->n_q_heads) * kD, nkv = static_cast<int64_t>(d->n_kv_heads) * kD;
   PromptParams p{};
   p.out = static_cast<uint16_t*>(out);
@@ -662,7 +662,7 @@ int gkv_prompt_mass(const gkv_prompt* d, const void* q, const void* k, const flo
   const std::vector<int> order = longest_first(d);
   if (order.empty()) return GKV_OK;
   if (!q || !k || !lse || !mass || misaligned(q, 16) || misaligned(k, 16) || misaligned(lse, 4) || misaligned(mass, 4)) return GKV_ERR_INVALID_ARG;
-  if (!here({q, k, lse, mass})) return GKV_ERR_INVALID_ARG;
+  if (!on_current_device({q, k, lse, mass})) return GKV_ERR_INVALID_ARG;
   const int64_t nq = static_cast<int64_t>(d->n_q_heads) * kD, nkv = static_cast<int64_t>(d->n_kv_heads) * kD;
   MassParams p{};
   p.lse = lse;
