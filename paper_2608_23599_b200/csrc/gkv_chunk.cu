@@ -10,10 +10,13 @@
 //
 // Work split.  gkv_chunk.h cuts all tiles' items into equal ranges, one per CTA; a block's place in its stream's walk is a golden-ratio
 // permutation of its age, so that a range holds every rung in its proportion.  Inside a CTA (one per SM: all 512 columns of tensor memory)
-//   warps 0-3, 4-7  softmax of even and odd steps: each four warps have an S and an O of their own, merged where a tile ends, so
-//                   that the tensor cores work on one step while the other's weights are made
-//   warps 8-15      fill the stages: 8-11 even, 12-15 odd steps, a warp each for half of the keys and half of the values
-//   warp 16         issues the products; warp 17 walks the items, publishes what each step is, and asks L2 for its bytes ahead of use
+//   warps 0-3, 4-7  softmax of even and odd steps: each four warps have an accumulator O of their own, merged where a tile ends
+//   warps 8-19      fill the key and value slots, four warps per step, three steps at once: a warp each for half of the keys or values
+//   warps 20, 23    issue O += P V and S = Q K^T.  S, keys, values and raw blocks lie in rings of three steps: a step's logits are there
+//                   when the four warps that take it have finished the step before.  (One thread for both was busy for 1150 cycles a step:
+//                   code that runs once a step comes from the instruction caches line by line.)
+//   warp 21         walks the items, publishes what each step is, and asks L2 for its bytes ahead of use
+//   warp 22         issues the bulk copies of quantised blocks as they are stored
 // Keys lie as [token][channel] rows.  Codes are stored in the order of warp-level fragments (gkv_layout.cuh), in which a lane's pairs run along
 // channels for keys and along tokens for values: dequantised values are written as [channel][token] rows, value rows of the other kinds as
 // [token][channel]; the product reads either (one bit of its descriptor).
@@ -30,16 +33,17 @@ namespace {
 
 using namespace tc;
 
-constexpr int kCThreads = 640;
-constexpr int kCStages = 6;                // an even number: even and odd steps have stages of their own
-constexpr int kCEntries = 16;              // steps published ahead, even as well
-constexpr int kCHalf = 16384;              // a stage: keys, then values
+constexpr int kCThreads = 768;
+constexpr int kCRing = 3;                  // steps that are filled at once, slots of keys and of values, buffers of S, raw blocks
+constexpr int kCEntries = 12;              // steps published ahead; a multiple of the ring and of the softmax halves
+constexpr int kCHalf = 16384;              // 64 keys or values
 constexpr int kCPanel = 8192;              // 64 channels of 64 rows
-constexpr int kCStageBytes = 2 * kCHalf;
-constexpr int kCLaunchRegs = 96, kCSoftRegs = 120, kCFillRegs = 96, kCOtherRegs = 48;
-static_assert(2 * kCSoftRegs + 2 * kCFillRegs + kCOtherRegs <= 5 * kCLaunchRegs, "a split draws on the launch's registers");
-// tensor memory
-constexpr uint32_t kCColQh = 0, kCColQb = 64, kCColO = 128, kCColS = 384;
+constexpr int kCRawBytes = 18432;          // a block as it is stored, up to 8 bits
+constexpr int kCLaunchRegs = 80, kCSoftRegs = 120, kCFillRegs = 64, kCOtherRegs = 48;
+static_assert(2 * kCSoftRegs + kCRing * kCFillRegs + kCOtherRegs <= 6 * kCLaunchRegs, "a split draws on the launch's registers");
+// tensor memory: the fp16 query, an accumulator per softmax half, the buffers of S
+constexpr uint32_t kCColQh = 0, kCColO = 64, kCColS = 320;
+static_assert(kCEntries % kCRing == 0 && kCEntries % 2 == 0 && kCColS + 64 * kCRing <= 512, "");
 
 enum : int32_t { kNone = 0, kCodes = 1, kRowsOf = 2, kCentroids = 3, kTileEnd = 4, kEnd = 5 };
 
@@ -56,11 +60,13 @@ struct alignas(16) Entry {
   alignas(16) float bias[kChunkKeys];      // and what their logits get
 };
 
-constexpr int kCOffEntry = kCStages * kCStageBytes;
+constexpr int kCOffK = 0, kCOffV = kCRing * kCHalf, kCOffQ = 2 * kCRing * kCHalf;      // (the bf16 query: two panels of 128 rows)
+constexpr int kCOffRaw = kCOffQ + kChunkRows * kD * 2;
+constexpr int kCOffEntry = kCOffRaw + kCRing * kCRawBytes;
 constexpr int kCOffMl = kCOffEntry + kCEntries * static_cast<int>(sizeof(Entry));
 constexpr int kCOffPend = kCOffMl + 2 * kChunkRows * 8;
 constexpr int kCOffBar = kCOffPend + 96 * 8;
-constexpr int kCBars = 2 * kCStages + 2 * kCEntries + 2 + 2 + 4;
+constexpr int kCBars = 6 * kCRing + 2 * kCEntries + 5;
 constexpr int kCSmem = kCOffBar + kCBars * 8 + 16 + 1024;
 static_assert(kCSmem <= 232448, "shared memory of a CTA");
 
@@ -89,12 +95,7 @@ struct ChunkLens {
 // ---- dequantisation ------------------------------------------------------------------------------
 __device__ __forceinline__ uint4 ldg128(const uint8_t* p) {
   uint4 v;
-  asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 ldg64(const uint8_t* p) {
-  uint2 v;
-  asm volatile("ld.global.nc.v2.u32 {%0,%1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  asm("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
 __device__ __forceinline__ __half2 h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
@@ -102,12 +103,44 @@ __device__ __forceinline__ uint32_t u32(__half2 h) { return *reinterpret_cast<ui
 // 1 / 2^p and -1024 / 2^p as fp16 pairs
 __device__ __forceinline__ constexpr uint32_t inv_pow2(int p) { return static_cast<uint32_t>(0x3c00 - (p << 10)) * 0x10001u; }
 __device__ __forceinline__ constexpr uint32_t neg_bias(int p) { return static_cast<uint32_t>(0xe400 - (p << 10)) * 0x10001u; }
-// The codes of fields (lane's MMA index s, register a) as an fp16 pair, exactly: or-ed into the mantissa of 1024 they are 1024 + code 2^p.
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(a));
+  return v;
+}
+// A lane's words of the MMA indices s = 2 j, 2 j + 1 of a 16-token tile: word 2 i + (a >> 1) at 8 bits, i at 4 bits, 0 (both) at 2 bits
+template <int BITS>
+__device__ __forceinline__ void lane_words(uint32_t tile, int j, int lane, uint32_t (&w)[4]) {
+  if constexpr (BITS == 8) {
+    const uint4 v = lds128(tile + (j * 32 + lane) * 16);
+    w[0] = v.x;
+    w[1] = v.y;
+    w[2] = v.z;
+    w[3] = v.w;
+  } else if constexpr (BITS == 4) {
+    const uint2 v = lds64(tile + ((j >> 1) * 32 + lane) * 16 + (j & 1) * 8);
+    w[0] = v.x;
+    w[1] = v.y;
+  } else {
+    w[0] = lds32(tile + lane * 16 + j * 4);
+  }
+}
+// The codes of fields (i = s & 1, register a) as an fp16 pair, exactly: or-ed into the mantissa of 1024 they are 1024 + code 2^p.
 template <int BITS, bool V>
-__device__ __forceinline__ __half2 code_pair(const uint32_t* w, int s, int a) {
+__device__ __forceinline__ __half2 code_pair(const uint32_t (&w)[4], int i, int a) {
   const int f = V ? ((a >> 1) | ((a & 1) << 1)) : a;
-  const int at = BITS == 8 ? 2 * s + (a >> 1) : BITS == 4 ? s : s >> 1;
-  int p = BITS == 8 ? 8 * (a & 1) : BITS == 4 ? 4 * f : 4 * (s & 1) + 2 * (f & 1) + 8 * (f >> 1);
+  const int at = BITS == 8 ? 2 * i + (a >> 1) : BITS == 4 ? i : 0;
+  int p = BITS == 8 ? 8 * (a & 1) : BITS == 4 ? 4 * f : 4 * i + 2 * (f & 1) + 8 * (f >> 1);
   uint32_t word = w[at];
   if (p + BITS > 10) {
     word >>= 8;
@@ -119,83 +152,73 @@ __device__ __forceinline__ __half2 code_pair(const uint32_t* w, int s, int a) {
 }
 __device__ __forceinline__ uint32_t pick(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Half of a block's keys (32 tokens): rows of the key tile.
+// Half of a block's keys (32 tokens) from the raw block in shared memory: rows of the key tile.  (The loop over the channels is not
+// unrolled further: three bit widths of keys and values unrolled whole are 60 KB of instructions, and a mixed context then waits for instructions
+// ten times as long as it issues them.)
 template <int BITS>
-__device__ __forceinline__ void fill_keys(const uint8_t* src, int half, uint32_t dst, int lane) {
-  constexpr int kChunks = BITS / 2;        // 16-byte pieces per lane and tile
+__device__ __forceinline__ void write_keys(uint32_t raw, int half, uint32_t dst, int lane) {
   const int r = lane >> 2, c4 = lane & 3;
-  uint32_t w[2][4 * kChunks];
+  const uint32_t row = dst + (half * 32 + r) * 128 + 4 * c4;
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {          // a slab of 32 channels: s = 2 j, 2 j + 1
+    const uint4 z = lds128(raw + (j * 4 + c4) * 32), sc = lds128(raw + (j * 4 + c4) * 32 + 16);
+    const uint32_t panel = row + (j >> 1) * kCPanel;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
+      uint32_t w[4];
+      lane_words<BITS>(raw + off_kc(BITS, t), j, lane, w);
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) *reinterpret_cast<uint4*>(&w[t][4 * i]) = ldg128(src + off_kc(BITS, t) + (i * 32 + lane) * 16);
-  uint32_t at[8];
-#pragma unroll
-  for (int c = 0; c < 8; ++c) at[c] = dst + (half * 32 + r) * 128 + ((c ^ r) << 4) + 4 * c4;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint4 z = ldg128(src + (j * 4 + c4) * 32), sc = ldg128(src + (j * 4 + c4) * 32 + 16);
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t at = panel + ((((j & 1) * 4 + 2 * i) ^ r) << 4);
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-          const int s = 2 * j + i, f = (a >> 1) * 2 + i;
-          const __half2 x = __hfma2(code_pair<BITS, false>(w[t], s, a), h2(pick(sc, f)), h2(pick(z, f)));
-          sts32(at[(s & 3) * 2 + (a >> 1)] + (s >> 2) * kCPanel + (16 * t + 8 * (a & 1)) * 128, u32(x));
+          const int f = (a >> 1) * 2 + i;
+          const __half2 v = __hfma2(code_pair<BITS, false>(w, i, a), h2(pick(sc, f)), h2(pick(z, f)));
+          sts32((a >> 1 ? at ^ 16u : at) + (16 * t + 8 * (a & 1)) * 128, u32(v));
         }
+      }
+    }
   }
 }
 // Half of a block's values (32 tokens): columns of the value tile, whose rows are channels.
 template <int BITS>
-__device__ __forceinline__ void fill_values(const uint8_t* src, int half, uint32_t dst, int lane) {
-  constexpr int kChunks = BITS / 2;
+__device__ __forceinline__ void write_values(uint32_t raw, int half, uint32_t dst, int lane) {
   const int r = lane >> 2, c4 = lane & 3;
+  const uint32_t row = dst + r * 128 + 4 * c4;
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {          // a group of 32 channels
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    uint32_t w[4 * kChunks];
+    for (int t = 0; t < 2; ++t) {
+      const uint2 sc = lds64(raw + off_vp(BITS, t) + c4 * 32 + j * 8), z = lds64(raw + off_vp(BITS, t) + 128 + (j * 4 + c4) * 8);
+      uint32_t w[4];
+      lane_words<BITS>(raw + off_vc(BITS, t), j, lane, w);
+      const uint32_t at = row + (((4 * half + 2 * t) ^ r) << 4) + j * 32 * 128;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) *reinterpret_cast<uint4*>(&w[4 * i]) = ldg128(src + off_vc(BITS, t) + (i * 32 + lane) * 16);
-    const uint8_t* vp = src + off_vp(BITS, t);
-    uint4 sc[2];
-    sc[0] = ldg128(vp + c4 * 32);
-    sc[1] = ldg128(vp + c4 * 32 + 16);
-    uint2 z[4];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) z[g] = ldg64(vp + 128 + (g * 4 + c4) * 8);
-    uint32_t at[2];
-#pragma unroll
-    for (int a = 0; a < 2; ++a) at[a] = dst + r * 128 + (((4 * half + 2 * t + a) ^ r) << 4) + 4 * c4;
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const int g = s >> 1, b = a >> 1;
-        const __half2 x = __hfma2(code_pair<BITS, true>(w, s, a), h2(pick(sc[g >> 1], (g & 1) * 2 + b)), h2(b ? z[g].y : z[g].x));
-        sts32(at[b] + (16 * s + 8 * (a & 1)) * 128, u32(x));
-      }
+        for (int a = 0; a < 4; ++a) {
+          const __half2 v = __hfma2(code_pair<BITS, true>(w, i, a), h2(a >> 1 ? sc.y : sc.x), h2(a >> 1 ? z.y : z.x));
+          sts32((a >> 1 ? at ^ 16u : at) + (16 * i + 8 * (a & 1)) * 128, u32(v));
+        }
+    }
   }
 }
-// Half of a step's rows, bf16, as they are; rows that are not there are zeros.
-template <bool GATHER>
-__device__ __forceinline__ void fill_rows(const uint8_t* base, uint32_t stride, const uint32_t* off, int rows, int half, uint32_t dst, int lane) {
+// A quarter of a step's rows, bf16, as they are; rows that are not there are zeros.
+__device__ __forceinline__ void fetch_rows(uint4 (&x)[8], const uint8_t* base, uint32_t stride, const uint32_t* off, int rows, int row0, int lane) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 2 * i + (lane >> 4);
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (row < rows) x[i] = ldg128(base + (off ? static_cast<size_t>(off[row]) * 256 : static_cast<size_t>(row) * stride) + (lane & 15) * 16);
+  }
+}
+__device__ __forceinline__ void write_rows(const uint4 (&x)[8], int row0, uint32_t dst, int lane) {
   const int c = lane & 15;
   const uint32_t panel = dst + (c >> 3) * kCPanel;
 #pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    uint4 x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = half * 32 + part * 16 + 2 * i + (lane >> 4);
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (row < rows) x[i] = ldg128(base + (GATHER ? static_cast<size_t>(off[row]) * 256 : static_cast<size_t>(row) * stride) + c * 16);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = half * 32 + part * 16 + 2 * i + (lane >> 4);
-      sts128(panel + row * 128 + (((c & 7) ^ (row & 7)) << 4), x[i]);
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 2 * i + (lane >> 4);
+    sts128(panel + row * 128 + (((c & 7) ^ (row & 7)) << 4), x[i]);
   }
 }
 
@@ -224,38 +247,45 @@ __global__ void __launch_bounds__(kCThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   Entry* const entries = reinterpret_cast<Entry*>(base + kCOffEntry);
   const uint32_t bars = smem + kCOffBar;
-  const uint32_t bar_full = bars, bar_empty = bar_full + 8 * kCStages, bar_put = bar_empty + 8 * kCStages, bar_got = bar_put + 8 * kCEntries;
-  const uint32_t bar_s = bar_got + 8 * kCEntries, bar_p = bar_s + 16, bar_q = bar_p + 16, bar_ml = bar_q + 8, bar_o = bar_ml + 8, bar_drain_mma = bar_o + 8;
+  // of a step, by place in the ring: keys are there; S is done (and its keys are free); weights and values are there; O is done (and its
+  // values and S are free); the raw block is there, is free
+  const uint32_t bar_k = bars, bar_s = bar_k + 8 * kCRing, bar_pv = bar_s + 8 * kCRing, bar_o = bar_pv + 8 * kCRing, bar_raw = bar_o + 8 * kCRing;
+  const uint32_t bar_rawfree = bar_raw + 8 * kCRing, bar_put = bar_rawfree + 8 * kCRing, bar_got = bar_put + 8 * kCEntries;
+  // of a tile: its queries are there; the halves' sums are there; all products are done
+  const uint32_t bar_q = bar_got + 8 * kCEntries, bar_ml = bar_q + 8, bar_tile = bar_ml + 8, bar_drain = bar_tile + 8;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kCOffBar + kCBars * 8);
   volatile uint32_t* const tmem_slot = abort + 1;
   const ChunkShape& sh = p.s;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kCStages; ++i) {
-      bar_init(bar_full + 8 * i, 4);
-      bar_init(bar_empty + 8 * i, 1);
+    for (int i = 0; i < kCRing; ++i) {
+      bar_init(bar_k + 8 * i, 2);
+      bar_init(bar_s + 8 * i, 1);
+      bar_init(bar_pv + 8 * i, 6);         // four warps of the softmax, two that fill the values
+      bar_init(bar_o + 8 * i, 1);
+      bar_init(bar_raw + 8 * i, 1);
+      bar_init(bar_rawfree + 8 * i, 4);
     }
     for (int i = 0; i < kCEntries; ++i) {
       bar_init(bar_put + 8 * i, 1);
-      bar_init(bar_got + 8 * i, 9);        // four warps that fill, four of the softmax, the products' thread
-    }
-    for (int i = 0; i < 2; ++i) {
-      bar_init(bar_s + 8 * i, 1);
-      bar_init(bar_p + 8 * i, 4);
+      bar_init(bar_got + 8 * i, 10);       // four warps that fill, four of the softmax, the O products', the raw blocks'
     }
     bar_init(bar_q, 8);
     bar_init(bar_ml, 8);
-    bar_init(bar_o, 1);
-    bar_init(bar_drain_mma, 1);
+    bar_init(bar_tile, 1);
+    for (int i = 0; i < 2; ++i) bar_init(bar_drain + 8 * i, 1);
     *abort = 0;
     bar_init_fence();
   }
-  if (warp == 16) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+  if (warp == 20) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
   tmem_before();
   __syncthreads();
   tmem_after();
   const uint32_t tmem = *tmem_slot;
-  auto wait_put = [&](int k) { return bar_wait(bar_put + 8 * (k % kCEntries), (k / kCEntries) & 1, abort); };
+  // Step k's turn of its place in a ring of n barriers.  (The softmax halves wait for every other step only; no turn that they leave out is
+  // unfinished then, and none that they wait for is overtaken: S(k) and S(k + 3) are issued in order, the second after O(k).)
+  auto wait_turn = [&](uint32_t bar, int n, int k) { return bar_wait(bar + 8 * (k % n), (k / n) & 1, abort); };
+  auto wait_put = [&](int k) { return wait_turn(bar_put, kCEntries, k); };
 
   if (warp < 8) {
     // ---- softmax ----
@@ -263,22 +293,24 @@ __global__ void __launch_bounds__(kCThreads, 1)
     constexpr int kCols = kChunkKeys / COPIES;           // columns of a step that a row of this copy takes
     const int w = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter) << 21);
-    const uint32_t s_tm = lanes + kCColS + 64 * w;
     const int vrow = quarter * 32 + lane;                // row of the tile, copies included
     const int row = vrow % (kChunkRows / COPIES), copy = vrow / (kChunkRows / COPIES);
     const int tok_in = row / sh.group, head_in = row % sh.group;
     const float c = p.scale_log2;
     float2* const ml = reinterpret_cast<float2*>(base + kCOffMl);
-    int steps = 0, seg = 0;
+    int seg = 0;
     bool ok = true, fresh = true, real = false, any_real = false;
-    int tok = 0, wrote = 0;
+    int tok = 0;
     float m = -INFINITY, l = 0.f;
     for (int k = w; ok; k += 2) {
       if (!(ok = wait_put(k))) break;
       const Entry& e = entries[k % kCEntries];
       const int kind = e.kind;
-      if (kind == kEnd) break;
-      if (fresh) {                                       // a tile begins: its rows go to tensor memory, as bf16 (warps 0-3) and fp16
+      if (kind == kEnd) {
+        if (lane == 0) bar_arrive(bar_pv + 8 * (k % kCRing));
+        break;
+      }
+      if (fresh) {                                       // a tile begins: its rows go to shared memory as bf16 (warps 0-3), to tensor memory as fp16
         const int tile = e.tile, rt = tile % sh.row_tiles, stream = tile / sh.row_tiles, b = stream / sh.n_kv_heads, h = stream % sh.n_kv_heads;
         tok = rt * sh.tile_tokens + tok_in;
         real = tok_in < sh.tile_tokens && tok < lens.len[N == 1 ? 0 : b];
@@ -287,20 +319,24 @@ __global__ void __launch_bounds__(kCThreads, 1)
             p.q + ((static_cast<size_t>(b) * sh.n_new + tok) * (sh.n_kv_heads * sh.group) + h * sh.group + head_in) * kD);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          uint32_t x[16];
+          uint4 v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint4 v = real ? src[4 * i + j] : make_uint4(0, 0, 0, 0);
-            x[4 * j] = v.x;
-            x[4 * j + 1] = v.y;
-            x[4 * j + 2] = v.z;
-            x[4 * j + 3] = v.w;
+          for (int j = 0; j < 4; ++j) v[j] = real ? src[4 * i + j] : make_uint4(0, 0, 0, 0);
+          if (w == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              sts128(smem + kCOffQ + (i >> 1) * (kChunkRows * 128) + vrow * 128 + ((((i & 1) * 4 + j) ^ (vrow & 7)) << 4), v[j]);
+          } else {
+            uint32_t x[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint32_t u = pick(v[j >> 2], j & 3);
+              x[j] = f16_pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+            }
+            tmem_st16(lanes + kCColQh + 16 * i, x);
           }
-          if (w)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = f16_pair(__uint_as_float(x[j] << 16), __uint_as_float(x[j] & 0xffff0000u));
-          tmem_st16(lanes + (w ? kCColQh : kCColQb) + 16 * i, x);
         }
+        fence_async();
         tmem_wait_st();
         tmem_before();
         __syncwarp();
@@ -308,15 +344,18 @@ __global__ void __launch_bounds__(kCThreads, 1)
         fresh = false;
         m = -INFINITY;
         l = 0.f;
-        wrote = 0;
       }
+      if (!(ok = wait_turn(bar_s, kCRing, k))) break;
+      const uint32_t s_tm = lanes + kCColS + 64 * (k % kCRing);
       if (kind == kTileEnd) {
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar_pv + 8 * (k % kCRing));      // (no weights)
         // ---- the two halves of the tile's steps are merged; these warps take channels 64 w .. + 63 ----
         ok = bar_wait(bar_q, seg & 1, abort);            // (everyone is past the previous tile's merge)
         ml[w * kChunkRows + vrow] = make_float2(m * c, l);
         __syncwarp();
         if (lane == 0) bar_arrive(bar_ml);
-        ok = ok && bar_wait(bar_ml, seg & 1, abort) && bar_wait(bar_o, seg & 1, abort);
+        ok = ok && bar_wait(bar_ml, seg & 1, abort) && bar_wait(bar_tile, seg & 1, abort);
         if (!ok) break;
         tmem_after();
         const float2 a = ml[vrow], b2 = ml[kChunkRows + vrow];
@@ -358,11 +397,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
         tmem_before();
         fresh = true;
         ++seg;
-      } else if (kind != kNone) {
-        ok = bar_wait(bar_s + 8 * w, steps & 1, abort);
-        if (!ok) break;
-        ++steps;
-        if (any_real) {
+      } else {
+        if (kind != kNone && any_real) {
           tmem_after();
           uint32_t x[kCols];
           if constexpr (COPIES == 4) {
@@ -408,6 +444,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
           const bool first = m == -INFINITY;
           const bool move = first ? top > -INFINITY : (top - m) * c > 8.f;
           if (__any_sync(0xffffffffu, move && !first)) {
+            // (S of this step was issued ahead of the O of the four warps' step before, which has to be complete now)
+            if (!(ok = wait_turn(bar_o, kCRing, k - 2))) break;
+            tmem_after();
             const float f = move && !first ? ex2((m - top) * c) : 1.f;
             l *= f;
 #pragma unroll 1
@@ -466,139 +505,165 @@ __global__ void __launch_bounds__(kCThreads, 1)
           tmem_wait_st();
           tmem_before();
         }
-        ++wrote;
         __syncwarp();
-        if (lane == 0) bar_arrive(bar_p + 8 * w);
+        if (lane == 0) bar_arrive(bar_pv + 8 * (k % kCRing));
       }
       __syncwarp();
       if (lane == 0) bar_arrive(bar_got + 8 * (k % kCEntries));
     }
-  } else if (warp < 16) {
-    // ---- stages ----
+  } else if (warp < 8 + 4 * kCRing) {
+    // ---- key and value slots ----
     fewer_regs<kCFillRegs>();
-    const int odd = (warp - 8) >> 2, half = warp & 1, is_v = (warp >> 1) & 1;
-    for (int k = odd;; k += 2) {
+    const int half = warp & 1, is_v = (warp >> 1) & 1, place = (warp - 8) >> 2;
+    const uint32_t bar_full = (is_v ? bar_pv : bar_k) + 8 * place, bar_free = is_v ? bar_o : bar_s;
+    const uint32_t dst = smem + (is_v ? kCOffV : kCOffK) + place * kCHalf;
+    for (int k = place;; k += kCRing) {
       if (!wait_put(k)) break;
       const Entry& e = entries[k % kCEntries];
-      const int kind = e.kind, stage = k % kCStages;
-      if (kind == kEnd) break;
-      if (k >= kCStages && !bar_wait(bar_empty + 8 * stage, (k / kCStages - 1) & 1, abort)) break;
-      const uint32_t dst = smem + stage * kCStageBytes + is_v * kCHalf;
-      if (kind == kCodes) {
-        const int level = e.level;
-        const uint8_t* src = p.arena + static_cast<size_t>(e.block) * 256 + half * half_bytes(level);
-        if (is_v) {
-          if (level == 4) fill_values<4>(src, half, dst, lane);
-          else if (level == 8) fill_values<8>(src, half, dst, lane);
-          else fill_values<2>(src, half, dst, lane);
-        } else {
-          if (level == 4) fill_keys<4>(src, half, dst, lane);
-          else if (level == 8) fill_keys<8>(src, half, dst, lane);
-          else fill_keys<2>(src, half, dst, lane);
-        }
-      } else if (kind == kRowsOf) {
-        fill_rows<false>(reinterpret_cast<const uint8_t*>(is_v ? e.v : e.k), e.stride, nullptr, e.rows, half, dst, lane);
-      } else if (kind == kCentroids) {
-        fill_rows<true>(p.arena + is_v * kRowBytes, 0, e.off, e.rows, half, dst, lane);
+      const int kind = e.kind;
+      auto slot_free = [&]() { return k < kCRing || wait_turn(bar_free, kCRing, k - kCRing); };
+      if (kind == kEnd) {
+        if (slot_free() && lane == 0) bar_arrive(bar_full);
+        break;
       }
+      bool ok;
+      if (kind == kRowsOf || kind == kCentroids) {
+        const bool gather = kind == kCentroids;
+        const uint8_t* src = gather ? p.arena + is_v * kRowBytes : reinterpret_cast<const uint8_t*>(is_v ? e.v : e.k);
+        uint4 x[8];
+        fetch_rows(x, src, e.stride, gather ? e.off : nullptr, e.rows, half * 32, lane);
+        if ((ok = slot_free())) {
+          write_rows(x, half * 32, dst, lane);
+          fetch_rows(x, src, e.stride, gather ? e.off : nullptr, e.rows, half * 32 + 16, lane);
+          write_rows(x, half * 32 + 16, dst, lane);
+        }
+        ok = ok && wait_turn(bar_raw, kCRing, k);
+      } else {
+        ok = wait_turn(bar_raw, kCRing, k) && slot_free();
+        if (ok && kind == kCodes) {
+          const int level = e.level;
+          const uint32_t src = smem + kCOffRaw + place * kCRawBytes + half * half_bytes(level);
+          if (is_v) {
+            if (level == 4) write_values<4>(src, half, dst, lane);
+            else if (level == 8) write_values<8>(src, half, dst, lane);
+            else write_values<2>(src, half, dst, lane);
+          } else {
+            if (level == 4) write_keys<4>(src, half, dst, lane);
+            else if (level == 8) write_keys<8>(src, half, dst, lane);
+            else write_keys<2>(src, half, dst, lane);
+          }
+        }
+      }
+      if (!ok) break;
       fence_async();
       __syncwarp();
       if (lane == 0) {
-        bar_arrive(bar_full + 8 * stage);
+        bar_arrive(bar_full);
+        bar_arrive(bar_rawfree + 8 * place);
         bar_arrive(bar_got + 8 * (k % kCEntries));
       }
     }
   } else {
     fewer_regs<kCOtherRegs>();
-    if (warp == 16) {
-      // ---- products ----
-      if (elect()) {
-        constexpr uint32_t id_qk_h = instr_desc(false, false, kChunkRows, kChunkKeys), id_qk_b = instr_desc(true, false, kChunkRows, kChunkKeys);
-        constexpr uint32_t id_pv_h = instr_desc(false, false, kChunkRows, kD), id_pv_b = instr_desc(true, true, kChunkRows, kD);
-        auto is_real = [&](int k) {
-          const int kind = entries[k % kCEntries].kind;
-          return kind == kCodes || kind == kRowsOf || kind == kCentroids;
-        };
-        auto wait_full = [&](int k) { return bar_wait(bar_full + 8 * (k % kCStages), (k / kCStages) & 1, abort); };
-        auto qk = [&](int k) {
-          const bool codes = entries[k % kCEntries].kind == kCodes;
-          const uint64_t b = smem_desc(smem + (k % kCStages) * kCStageBytes, 16);
-          const uint32_t a = tmem + (codes ? kCColQh : kCColQb), id = codes ? id_qk_h : id_qk_b;
-          for (int i = 0; i < kD / 16; ++i) mma_ts(tmem + kCColS + 64 * (k & 1), a + 8 * i, b + (((i >> 2) * kCPanel + (i & 3) * 32) >> 4), id, i > 0);
-          mma_commit(bar_s + 8 * (k & 1));
-        };
-        auto pv = [&](int k, bool first) {
-          const bool codes = entries[k % kCEntries].kind == kCodes;
-          const uint32_t v = smem + (k % kCStages) * kCStageBytes + kCHalf;
-          const uint64_t b = codes ? smem_desc(v, 16) : smem_desc(v, kCPanel);
-          const uint32_t step = (codes ? 32 : 16 * 128) >> 4, id = codes ? id_pv_h : id_pv_b;
-          for (int i = 0; i < kChunkKeys / 16; ++i) mma_ts(tmem + kCColO + 128 * (k & 1), tmem + kCColS + 64 * (k & 1) + 8 * i, b + i * step, id, !first || i > 0);
-        };
-        bool ok = true, fresh = true, first[2] = {true, true};
-        int seg = 0, done[2] = {0, 0};
-        for (int k = 0;; k += 2) {
-          ok = wait_put(k) && wait_put(k + 1);
-          if (!ok) break;
-          const int kind = entries[k % kCEntries].kind;
-          if (kind == kEnd) break;
-          const bool begin = fresh;
-          if (fresh) {
-            ok = bar_wait(bar_q, seg & 1, abort);
-            if (!ok) break;
-            tmem_after();
-            fresh = false;
-            first[0] = first[1] = true;
-          }
-          if (kind == kTileEnd) {
-            ok = wait_full(k) && wait_full(k + 1);       // (nothing was filled: the stages' turns go on)
-            if (!ok) break;
-            mma_commit(bar_o);
-            for (int t = 0; t < 2; ++t) {
-              mma_commit(bar_empty + 8 * ((k + t) % kCStages));
-              bar_arrive(bar_got + 8 * ((k + t) % kCEntries));
-            }
-            fresh = true;
-            ++seg;
-            continue;
-          }
-          if (begin)
-            for (int t = 0; t < 2 && ok; ++t) {
-              ok = wait_full(k + t);
-              if (ok && is_real(k + t)) {
-                tmem_after();
-                qk(k + t);
-              }
-            }
-          ok = ok && wait_put(k + 2) && wait_put(k + 3);
-          if (!ok) break;
-          const int next = entries[(k + 2) % kCEntries].kind;
-          const bool more = next != kTileEnd && next != kEnd;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (is_real(k + t)) {
-              ok = bar_wait(bar_p + 8 * t, done[t] & 1, abort);
-              if (!ok) break;
-              ++done[t];
-              tmem_after();
-              pv(k + t, first[t]);
-              first[t] = false;
-            }
-            mma_commit(bar_empty + 8 * ((k + t) % kCStages));
-            bar_arrive(bar_got + 8 * ((k + t) % kCEntries));
-            if (more) {
-              ok = wait_full(k + 2 + t);
-              if (ok && is_real(k + 2 + t)) {
-                tmem_after();
-                qk(k + 2 + t);
-              }
-            }
-          }
-          if (!ok) break;
+    if (warp == 23) {
+      // ---- S = Q K^T ----  (whole warps walk, one lane issues: addresses stay in uniform registers)
+      constexpr uint32_t id_h = instr_desc(false, false, kChunkRows, kChunkKeys), id_b = instr_desc(true, false, kChunkRows, kChunkKeys);
+      const bool leader = elect();
+      const uint64_t q = smem_desc(smem + kCOffQ, 16);
+      int seg = 0;
+      bool ok = true, begin = true;
+      for (int k = 0;; ++k) {
+        const int place = k % kCRing;
+        ok = wait_turn(bar_k, kCRing, k) && (k < kCRing || wait_turn(bar_o, kCRing, k - kCRing));
+        if (!ok) break;
+        const int kind = entries[k % kCEntries].kind;
+        if (kind == kEnd) break;
+        if (begin) {
+          if (!(ok = bar_wait(bar_q, seg & 1, abort))) break;
+          ++seg;
         }
-        mma_commit(bar_drain_mma);                       // products in flight end before tensor memory is given back
-        bar_drain(bar_drain_mma, 0);
-        if (!ok || *abort) atomicOr(p.status, kStatusInternal);
+        begin = kind == kTileEnd && (k & 1);
+        tmem_after();
+        if (leader) {
+          const uint64_t b = smem_desc(smem + kCOffK + place * kCHalf, 16);
+          const uint32_t d = tmem + kCColS + 64 * place;
+          if (kind == kCodes) {
+#pragma unroll
+            for (int i = 0; i < kD / 16; ++i) mma_ts(d, tmem + kCColQh + 8 * i, b + (((i >> 2) * kCPanel + (i & 3) * 32) >> 4), id_h, i > 0);
+          } else if (kind == kRowsOf || kind == kCentroids) {
+#pragma unroll
+            for (int i = 0; i < kD / 16; ++i)
+              mma_ss(d, q + (((i >> 2) * (kChunkRows * 128) + (i & 3) * 32) >> 4), b + (((i >> 2) * kCPanel + (i & 3) * 32) >> 4), id_b, i > 0);
+          }
+          mma_commit(bar_s + 8 * place);
+        }
+        __syncwarp();
       }
-    } else if (warp == 17) {
+      if (leader) {
+        mma_commit(bar_drain);                           // products in flight end before tensor memory is given back
+        tc::bar_drain(bar_drain, 0);
+        if (!ok) atomicOr(p.status, kStatusInternal);
+      }
+    } else if (warp == 20) {
+      // ---- O += P V ----
+      constexpr uint32_t id_h = instr_desc(false, false, kChunkRows, kD), id_b = instr_desc(true, true, kChunkRows, kD);
+      const bool leader = elect();
+      bool ok = true, some[2] = {false, false};          // the halves' O hold something
+      for (int k = 0;; ++k) {
+        const int place = k % kCRing;
+        if (!(ok = wait_turn(bar_pv, kCRing, k))) break;
+        const int kind = entries[k % kCEntries].kind;
+        if (kind == kEnd) break;
+        tmem_after();
+        const bool real = kind == kCodes || kind == kRowsOf || kind == kCentroids;
+        if (leader) {
+          const uint32_t v = smem + kCOffV + place * kCHalf, d = tmem + kCColO + 128 * (k & 1), a = tmem + kCColS + 64 * place;
+          if (kind == kCodes) {
+            const uint64_t b = smem_desc(v, 16);
+#pragma unroll
+            for (int i = 0; i < kChunkKeys / 16; ++i) mma_ts(d, a + 8 * i, b + i * (32 >> 4), id_h, i > 0 || some[k & 1]);
+          } else if (real) {
+            const uint64_t b = smem_desc(v, kCPanel);
+#pragma unroll
+            for (int i = 0; i < kChunkKeys / 16; ++i) mma_ts(d, a + 8 * i, b + i * (16 * 128 >> 4), id_b, i > 0 || some[k & 1]);
+          } else if (kind == kTileEnd && (k & 1)) {
+            mma_commit(bar_tile);
+          }
+          mma_commit(bar_o + 8 * place);
+          bar_arrive(bar_got + 8 * (k % kCEntries));
+        }
+        __syncwarp();
+        if (real) some[k & 1] = true;
+        if (kind == kTileEnd) some[k & 1] = false;
+      }
+      if (leader) {
+        mma_commit(bar_drain + 8);
+        tc::bar_drain(bar_drain + 8, 0);
+        if (!ok) atomicOr(p.status, kStatusInternal);
+      }
+    } else if (warp == 22) {
+      // ---- raw blocks, a few steps ahead of the stages ----
+      if (elect()) {
+        int k = 0;
+        for (;; ++k) {
+          if (!wait_put(k)) break;
+          const Entry& e = entries[k % kCEntries];
+          if (e.kind == kEnd) break;
+          const int slot = k % kCRing;
+          if (k >= kCRing && !wait_turn(bar_rawfree, kCRing, k - kCRing)) break;
+          if (e.kind == kCodes) {
+            const uint32_t bytes = slot_bytes(e.level);
+            bar_expect(bar_raw + 8 * slot, bytes);
+            bulk_load(smem + kCOffRaw + slot * kCRawBytes, p.arena + static_cast<size_t>(e.block) * 256, bytes, bar_raw + 8 * slot);
+          } else {
+            bar_arrive(bar_raw + 8 * slot);
+          }
+          bar_arrive(bar_got + 8 * (k % kCEntries));
+        }
+        if (*abort)                              // what is on its way arrives before the CTA leaves
+          for (int i = max(0, k - kCRing); i < k; ++i) tc::bar_drain(bar_raw + 8 * (i % kCRing), (i / kCRing) & 1);
+      }
+    } else if (warp == 21) {
       // ---- walk ----
       uint32_t* const pend_off = reinterpret_cast<uint32_t*>(base + kCOffPend);
       float* const pend_bias = reinterpret_cast<float*>(pend_off + 96);
@@ -607,7 +672,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
       // the next step's entry, once its place is free; everyone's lane sees the same arguments
       auto put = [&](const Entry& head, bool centroids) {
         if (!ok) return;
-        if (k >= kCEntries) ok = bar_wait(bar_got + 8 * (k % kCEntries), (k / kCEntries - 1) & 1, abort);
+        if (k >= kCEntries) ok = wait_turn(bar_got, kCEntries, k - kCEntries);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) return;
         Entry& e = entries[k % kCEntries];
@@ -747,14 +812,13 @@ __global__ void __launch_bounds__(kCThreads, 1)
       }
       Entry x{};
       x.kind = kEnd;
-      put(x, false);
-      put(x, false);
+      for (int i = 0; i < kCRing; ++i) put(x, false);      // everyone who walks the steps meets one
     }
   }
   __syncwarp();
   tmem_before();
   __syncthreads();
-  if (warp == 16) tmem_dealloc(tmem, 512);
+  if (warp == 20) tmem_dealloc(tmem, 512);
 }
 
 // Merges the slots of tiles that were cut (or hold copies of their rows): a warp per row, four channels per lane, slots in order.

@@ -58,6 +58,7 @@ def run(c, q, k, v, lengths=None, **kw):
     lse = torch.full(q.shape[:3], 7.0, device=DEV)
     c.gkv_chunk_attn(0, q.to(DEV), k.to(DEV), v.to(DEV), out, lse=lse, lengths=lengths, **kw)
     torch.cuda.synchronize()
+    c.gkv_bits_report(0)               # (raises where a kernel gave up a wait)
     return out, lse
 
 
