@@ -129,8 +129,15 @@ def load():
     from . import _gkv_call
     _gkv_call.bind(*(C.cast(f, vp).value for f in (lib.gkv_append_demote, lib.gkv_decode_attn, lib.gkv_decode_attn_observe,
                                                    lib.gkv_quest_select)), vp)
+    _gkv_call.bind_rows(*(C.cast(f, vp).value for f in (lib.gkv_prompt_attn, lib.gkv_prompt_mass, lib.gkv_chunk_attn)), torch.Tensor, torch.bfloat16,
+                        torch.float32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
     _lib, _call = lib, _gkv_call
     return lib
+
+
+def _loaded():
+    load()
+    return _call
 
 
 def strerror(status: int) -> str:
@@ -267,6 +274,11 @@ def gkv_prompt_attn(q, k, v, out, offsets, lse=None, softmax_scale=0.0):
     """Causal attention of packed prompts: q, out cuda bf16 [rows][n_q_heads][128], k, v cuda bf16 [rows][n_kv_heads][128]
     (rows may be slices of a fused projection), offsets: host row numbers, sequence s = rows [offsets[s], offsets[s + 1]);
     lse: cuda fp32 [rows][n_q_heads] or None.  Rows of no sequence are left as they are."""
+    rc = (_call or _loaded()).prompt_attn(q, k, v, out, offsets, lse, softmax_scale)
+    if rc == OK:
+        return rc
+    if rc is not NotImplemented:
+        return _check(rc, "gkv_prompt_attn")
     qs, ks = _rows(q, "q", torch.bfloat16), _rows(k, "k", torch.bfloat16)
     vs, os_ = _rows(v, "v", torch.bfloat16, k.shape), _rows(out, "out", torch.bfloat16, q.shape)
     if k.shape[0] != q.shape[0]:
@@ -283,6 +295,11 @@ def gkv_prompt_mass(q, k, lse, mass, offsets, n_obs, softmax_scale=0.0):
     """Attention masses of prompt tokens under the newest n_obs queries of their sequence: q, k, offsets as for
     gkv_prompt_attn, lse the log-sum-exp that it wrote; mass: cuda fp32, [n_kv_heads][length] sequence after sequence (for
     sequences of one length the token_mass that gkv_append_demote takes)."""
+    rc = (_call or _loaded()).prompt_mass(q, k, lse, mass, mass.dim() if isinstance(mass, torch.Tensor) else 0, offsets, n_obs, softmax_scale)
+    if rc == OK:
+        return rc
+    if rc is not NotImplemented:
+        return _check(rc, "gkv_prompt_mass")
     qs, ks = _rows(q, "q", torch.bfloat16), _rows(k, "k", torch.bfloat16)
     if k.shape[0] != q.shape[0]:
         raise ValueError(f"k: {k.shape[0]} rows, not {q.shape[0]}")
@@ -309,8 +326,10 @@ class Cache:
         h = C.c_void_p()
         _check(load().gkv_create(C.byref(cfg), self._arena_ptr, nbytes, C.byref(h)), "gkv_create")
         self.handle = h
+        self._chunk_bytes, self._chunk_spaces = {}, {}
 
     def close(self):
+        self._chunk_spaces = {}
         if getattr(self, "handle", None):
             load().gkv_destroy(self.handle)
             self.handle = None
@@ -368,7 +387,19 @@ class Cache:
         q, out: cuda bf16 [B][n_new][Hq][128]; k_new, v_new: cuda bf16 [B][n_new][Hkv][128]; lse: cuda fp32 [B][n_new][Hq] or
         None; lengths: host ints [B] (rows from there on are left as they are) or None; workspace: a cuda tensor of
         gkv_chunk_workspace_bytes bytes, or None (one is taken from torch's allocator for the call)."""
-        b, hq, hkv, dev = self.cfg.batch, self.cfg.n_q_heads, self.cfg.n_kv_heads, self.arena.device
+        cfg = self.cfg
+        ws, keep = (workspace, None) if workspace is not None else self._chunk_workspace(q)
+        if isinstance(ws, torch.Tensor):
+            ws = (ws.data_ptr(), ws.numel() * ws.element_size()) if ws.device == self.arena.device and ws.is_contiguous() else None
+        if ws is not None:
+            rc = _call.chunk(self.handle, layer, q, k_new, v_new, out, lse, lengths, ws[0], ws[1], cfg.batch, cfg.n_q_heads, cfg.n_kv_heads,
+                             self.stream_handle, self.arena.device.index)
+            if rc == OK:
+                return rc
+            if rc is not NotImplemented:
+                return _check(rc, "gkv_chunk_attn")
+        # the long way: names what is wrong, takes lengths of any kind, and a device that is not the current one
+        b, hq, hkv, dev = cfg.batch, cfg.n_q_heads, cfg.n_kv_heads, self.arena.device
         n = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 4 else 0
         for t, name, h, dt in ((q, "q", hq, torch.bfloat16), (k_new, "k_new", hkv, torch.bfloat16), (v_new, "v_new", hkv, torch.bfloat16),
                                (out, "out", hq, torch.bfloat16), (lse, "lse", hq, torch.float32)):
@@ -377,28 +408,44 @@ class Cache:
             shape = (b, n, h) if name == "lse" else (b, n, h, 128)
             if not isinstance(t, torch.Tensor) or tuple(t.shape) != shape or t.dtype != dt or t.device != dev or not t.is_contiguous():
                 raise ValueError(f"{name}: a contiguous {dt} tensor {list(shape)} on {dev} is needed")
+        if ws is None:
+            raise ValueError(f"workspace: a contiguous tensor on {dev} is needed")
         ln = None
         if lengths is not None:
             ln = np.ascontiguousarray(lengths, dtype=np.int32)
             if ln.shape != (b,):
                 raise ValueError(f"lengths: {b} of them are needed")
 
-        if workspace is not None and (not isinstance(workspace, torch.Tensor) or workspace.device != dev or not workspace.is_contiguous()):
-            raise ValueError(f"workspace: a contiguous tensor on {dev} is needed")
-
         def call(st):
-            ws = workspace
-            if self.stream_handle is not None and self.stream_handle != st:
-                st = self.stream_handle
-                if ws is None:      # memory that is free again in the order of the stream that uses it
-                    with torch.cuda.stream(torch.cuda.ExternalStream(st, device=dev)):
-                        ws = torch.empty(self.gkv_chunk_workspace_bytes(n), dtype=torch.uint8, device=dev)
-            if ws is None:
-                ws = torch.empty(self.gkv_chunk_workspace_bytes(n), dtype=torch.uint8, device=dev)
             return load().gkv_chunk_attn(self.handle, layer, _ptr(q), _ptr(k_new), _ptr(v_new), n, None if ln is None else ln.ctypes.data,
-                                         _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), st)
+                                         _ptr(out), _ptr(lse), ws[0], ws[1], st if self.stream_handle is None else self.stream_handle)
         rc = _on(dev, call)
         return rc if rc == OK else _check(rc, "gkv_chunk_attn")
+
+    def _chunk_workspace(self, q):
+        """(address, bytes) of a workspace for a chunk like q, and its owner.  One is kept per stream, whose calls follow one another; a captured
+        call gets memory of its graph's own."""
+        n = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 4 else 0
+        if n == 0:
+            return (None, 0), None
+        need = self._chunk_bytes.get(n)
+        if need is None:
+            need = self._chunk_bytes[n] = self.gkv_chunk_workspace_bytes(n)
+        dev, handle = self.arena.device, self.stream_handle
+        st = torch._C._cuda_getCurrentRawStream(dev.index) if handle is None else handle
+        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        kept = None if capturing else self._chunk_spaces.get(st)
+        if kept is None or kept[0][1] < need:
+            with torch.cuda.device(dev):
+                if handle is None:
+                    t = torch.empty(need, dtype=torch.uint8, device=dev)
+                else:      # memory that is free again in the order of the stream that uses it
+                    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=dev)):
+                        t = torch.empty(need, dtype=torch.uint8, device=dev)
+            kept = (t.data_ptr(), need), t
+            if not capturing:
+                self._chunk_spaces[st] = kept
+        return kept
 
     def gkv_debug_export_bounds(self, layer):
         """Per-block certificate bounds as numpy [batch][n_kv_heads][n_closed][4] (kappa, delta, max |v|, 0)."""
