@@ -1965,6 +1965,7 @@ ChunkShape chunk_of(const gkv_cache* c, int32_t n_new) {
   s.group = c->group;
   s.n_new = n_new;
   chunk_shape(&s);
+  s.item_keys = kChunkKeys;
   return s;
 }
 }  // namespace
@@ -1995,13 +1996,16 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
   const LayerState& L = c->layers[layer];
   ChunkCall call{};
   call.shape = chunk_of(c, n_new);
-  call.shape.n_closed = L.n_closed;
-  call.shape.n_tail = L.n_tail;
+  call.n_closed = L.n_closed;
+  call.n_tail = L.n_tail;
   if (L.has_residual)
-    for (int s = 0; s < c->n_streams; ++s) call.shape.res_groups = std::max(call.shape.res_groups, (L.res_count_h[s] + kChunkKeys - 1) / kChunkKeys);
+    for (int s = 0; s < c->n_streams; ++s) call.res_rows = std::max(call.res_rows, L.res_count_h[s]);
+  const bool few = static_cast<int64_t>(n_new) * c->group <= kVerifyRows;
+  call.shape.cache_items = L.n_closed + (L.n_tail > 0) + (call.res_rows + kChunkKeys - 1) / kChunkKeys;
+  if (few) verify_shape(&call.shape, L.n_closed, L.n_tail, call.res_rows);
   ChunkCuts cuts;
   ChunkMerge merge;
-  const int slots = chunk_plan(call.shape, len, &cuts, &merge);
+  const int slots = chunk_plan(call.shape, len, few ? 6 : 4, &cuts, &merge);
   if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
   call.arena = c->arena;
   call.table = L.table_d;
@@ -2016,7 +2020,7 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
   call.workspace = static_cast<float*>(workspace);
   call.status = c->status_d;
   call.scale = c->scale;
-  CK(c, launch_chunk(call, cuts, merge, len, static_cast<cudaStream_t>(stream)));
+  CK(c, (few ? launch_verify : launch_chunk)(call, cuts, merge, len, static_cast<cudaStream_t>(stream)));
   return GKV_OK;
 }
 

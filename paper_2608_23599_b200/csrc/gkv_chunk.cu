@@ -84,12 +84,9 @@ struct ChunkParams {
   float2* part_ml;           // [slot][128]: reference (log2), sum
   uint32_t* status;
   int32_t table_stride, walk;      // walk: the permutation's step, coprime to the closed blocks
+  int32_t n_closed, n_tail, res_groups;
   float scale_log2;
   ChunkShape s;
-};
-template <int N>
-struct ChunkLens {
-  int32_t len[N];
 };
 
 // ---- dequantisation ------------------------------------------------------------------------------
@@ -713,7 +710,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         head.tile = tile;
         head.causal = -1;
         const TableEntry* table = p.table + static_cast<size_t>(stream) * p.table_stride;
-        const int last_block = min(end, sh.n_closed);
+        const int last_block = min(end, p.n_closed);
         auto centroid_step = [&]() {
           Entry x = head;
           x.kind = kCentroids;
@@ -729,7 +726,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         };
         for (int i = begin; ok && i < last_block; i += 32) {
           TableEntry t{};
-          if (i + lane < last_block) t = table[static_cast<uint64_t>(i + lane) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(sh.n_closed)];
+          if (i + lane < last_block) t = table[static_cast<uint64_t>(i + lane) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(p.n_closed)];
           const bool cent = t.level == 1;
           const uint32_t cents = __ballot_sync(0xffffffffu, cent);
           if (cent) {
@@ -766,19 +763,19 @@ __global__ void __launch_bounds__(kCThreads, 1)
           }
         }
         if (ok && pend > 0) centroid_step();
-        int i = max(begin, sh.n_closed);
-        if (ok && sh.n_tail > 0 && i == sh.n_closed && i < end) {
+        int i = max(begin, p.n_closed);
+        if (ok && p.n_tail > 0 && i == p.n_closed && i < end) {
           Entry x = head;
-          const uint8_t* at = p.arena + static_cast<size_t>(table[sh.n_closed].off256) * 256;
+          const uint8_t* at = p.arena + static_cast<size_t>(table[p.n_closed].off256) * 256;
           x.kind = kRowsOf;
-          x.rows = sh.n_tail;
+          x.rows = p.n_tail;
           x.k = reinterpret_cast<uint64_t>(at);
           x.v = reinterpret_cast<uint64_t>(at + kBlock * kRowBytes);
           x.stride = kRowBytes;
           put(x, false);
           ++i;
         }
-        const int res0 = sh.n_closed + (sh.n_tail > 0), new0 = res0 + sh.res_groups;
+        const int res0 = p.n_closed + (p.n_tail > 0), new0 = res0 + p.res_groups;
         for (; ok && i < min(end, new0); ++i) {
           const int row0 = (i - res0) * kChunkKeys, n = min(kChunkKeys, p.res_count[stream] - row0);
           if (n <= 0) continue;
@@ -861,30 +858,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
   if (p.lse && lane == 0) p.lse[at] = (top + lg2(sum)) * kLn2;
 }
 
-template <int COPIES, int N>
-cudaError_t launch_as(const ChunkParams& p, const ChunkCuts& cuts, const ChunkMerge& merge, const ChunkLens<N>& lens, cudaStream_t st) {
-  static std::atomic<uint64_t> done{0};
-  cudaError_t e = raise_smem_limit(chunk_kernel<COPIES, N>, kCSmem, done);
-  if (e != cudaSuccess) return e;
-  chunk_kernel<COPIES, N><<<cuts.n, kCThreads, kCSmem, st>>>(p, cuts, lens);
-  if ((e = cudaGetLastError()) != cudaSuccess || merge.n == 0) return e;
-  chunk_merge_kernel<N><<<dim3((p.s.tile_tokens * p.s.group + 7) / 8, merge.n), 256, 0, st>>>(p, merge, lens);
-  return cudaGetLastError();
-}
-template <int N>
-cudaError_t launch_lens(const ChunkParams& p, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
-  ChunkLens<N> lens;
-  for (int b = 0; b < (N == 1 ? 1 : p.s.batch); ++b) lens.len[b] = len ? len[b] : p.s.n_new;
-  if (p.s.copies == 4) return launch_as<4, N>(p, cuts, merge, lens, st);
-  if (p.s.copies == 2) return launch_as<2, N>(p, cuts, merge, lens, st);
-  return launch_as<1, N>(p, cuts, merge, lens, st);
-}
-
-}  // namespace
-
-// len: HOST [batch], or null where every sequence has n_new rows.
-cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
-  if (cuts.n == 0) return cudaSuccess;
+ChunkParams params_of(const ChunkCall& call, int slots) {
   ChunkParams p{};
   p.arena = call.arena;
   p.table = call.table;
@@ -896,27 +870,57 @@ cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const Chu
   p.out = call.out;
   p.lse = call.lse;
   p.part_o = call.workspace;
-  p.part_ml = reinterpret_cast<float2*>(call.workspace + static_cast<size_t>(merge.slot[merge.n]) * kChunkRows * kD);
+  p.part_ml = reinterpret_cast<float2*>(call.workspace + static_cast<size_t>(slots) * kChunkRows * kD);
   p.status = call.status;
   p.table_stride = call.table_stride;
+  p.walk = chunk_walk(call.n_closed);
+  p.n_closed = call.n_closed;
+  p.n_tail = call.n_tail;
+  p.res_groups = (call.res_rows + kChunkKeys - 1) / kChunkKeys;
   p.scale_log2 = call.scale * kLog2e;
   p.s = call.shape;
-  // about 0.618 of the blocks, coprime to their number
-  p.walk = 1;
-  if (p.s.n_closed > 2) {
-    auto gcd = [](int a, int b) {
-      while (b) {
-        const int t = a % b;
-        a = b;
-        b = t;
-      }
-      return a;
-    };
-    p.walk = static_cast<int>(p.s.n_closed * 0.6180339887);
-    while (gcd(p.walk, p.s.n_closed) != 1) ++p.walk;
-  }
-  if (!len || p.s.batch == 1) return launch_lens<1>(p, cuts, merge, len, st);
-  return launch_lens<kChunkMaxBatch>(p, cuts, merge, len, st);
+  return p;
+}
+template <int N>
+ChunkLens<N> lens_of(const ChunkCall& call, const int32_t* len) {
+  ChunkLens<N> lens;
+  for (int b = 0; b < (N == 1 ? 1 : call.shape.batch); ++b) lens.len[b] = len ? len[b] : call.shape.n_new;
+  return lens;
+}
+
+template <int COPIES, int N>
+cudaError_t launch_as(const ChunkParams& p, const ChunkCuts& cuts, const ChunkLens<N>& lens, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = raise_smem_limit(chunk_kernel<COPIES, N>, kCSmem, done);
+  if (e != cudaSuccess) return e;
+  chunk_kernel<COPIES, N><<<cuts.n, kCThreads, kCSmem, st>>>(p, cuts, lens);
+  return cudaGetLastError();
+}
+template <int N>
+cudaError_t launch_lens(const ChunkParams& p, const ChunkCuts& cuts, const ChunkLens<N>& lens, cudaStream_t st) {
+  if (p.s.copies == 4) return launch_as<4, N>(p, cuts, lens, st);
+  if (p.s.copies == 2) return launch_as<2, N>(p, cuts, lens, st);
+  return launch_as<1, N>(p, cuts, lens, st);
+}
+bool one_len(const ChunkCall& call, const int32_t* len) { return !len || call.shape.batch == 1; }
+
+}  // namespace
+
+// len: HOST [batch], or null where every sequence has n_new rows.
+cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
+  if (cuts.n == 0) return cudaSuccess;
+  const ChunkParams p = params_of(call, merge.slot[merge.n]);
+  const cudaError_t e = one_len(call, len) ? launch_lens<1>(p, cuts, lens_of<1>(call, len), st) : launch_lens<kChunkMaxBatch>(p, cuts, lens_of<kChunkMaxBatch>(call, len), st);
+  return e != cudaSuccess ? e : launch_chunk_merge(call, merge, len, st);
+}
+
+cudaError_t launch_chunk_merge(const ChunkCall& call, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
+  if (merge.n == 0) return cudaSuccess;
+  const ChunkParams p = params_of(call, merge.slot[merge.n]);
+  const dim3 grid((std::min(p.s.tile_tokens * p.s.group, kChunkRows / p.s.copies) + 7) / 8, merge.n);
+  if (one_len(call, len)) chunk_merge_kernel<1><<<grid, 256, 0, st>>>(p, merge, lens_of<1>(call, len));
+  else chunk_merge_kernel<kChunkMaxBatch><<<grid, 256, 0, st>>>(p, merge, lens_of<kChunkMaxBatch>(call, len));
+  return cudaGetLastError();
 }
 
 }  // namespace gkv

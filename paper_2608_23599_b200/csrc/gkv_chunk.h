@@ -1,10 +1,10 @@
 // The work of a chunk call (attention of several new tokens per sequence over the graded cache) and how it is cut into CTAs.
 // Host code without CUDA calls: it runs on a host alone as well.
 //
-// A tile is up to 128 rows of one stream: the query heads of `tile_tokens` consecutive new tokens.  It walks the stream's items: every
-// closed block, the partial block, the groups of 64 exact residual rows, and the chunk's own rows in groups of 64 as far as the tile's
-// last token sees them.  All tiles' items are laid end to end and cut into equal ranges, one per CTA, so a CTA has the end of one
-// tile, whole tiles, and the beginning of another.  A tile that was cut leaves partial results in slots; the slots of a tile follow one another.
+// A tile is up to 128 rows of one stream: the query heads of `tile_tokens` consecutive new tokens.  It walks the stream's items: those of
+// the cache, then the chunk's own rows in groups of `item_keys` as far as the tile's last token sees them.  All tiles' items are laid end to end and
+// cut into equal ranges, one per CTA, so a CTA has the end of one tile, whole tiles, and the beginning of another.  A tile that was cut leaves
+// partial results in slots; the slots of a tile follow one another.
 #pragma once
 #include <stdint.h>
 
@@ -15,7 +15,6 @@ namespace gkv {
 constexpr int kChunkRows = 128;            // rows of a tile
 constexpr int kChunkKeys = 64;             // keys of a step
 constexpr int kChunkCtas = 148;            // one CTA per SM: all of its tensor memory, most of its shared memory
-constexpr int kChunkMinItems = 4;          // items that a CTA is worth starting for
 constexpr int kChunkParts = 2 * kChunkCtas;      // most slots of a call, and most tiles to be merged
 constexpr int kChunkSlotFloats = kChunkRows * (128 + 2);
 
@@ -23,7 +22,7 @@ constexpr int kChunkMaxBatch = 1024;       // sequences of a call with lengths o
 
 struct ChunkShape {
   int32_t batch, n_kv_heads, group, n_new;
-  int32_t n_closed, n_tail, res_groups;      // residual groups: of the stream that has most
+  int32_t cache_items, item_keys;
   int32_t tile_tokens, row_tiles, copies;    // copies: see chunk_shape
 };
 
@@ -35,7 +34,7 @@ __host__ __device__
 inline int chunk_items(const ChunkShape& s, int len, int rt) {
   if (rt * s.tile_tokens >= len) return 0;
   const int seen = (rt + 1) * s.tile_tokens < len ? (rt + 1) * s.tile_tokens : len;
-  return s.n_closed + (s.n_tail > 0) + s.res_groups + (seen + kChunkKeys - 1) / kChunkKeys;
+  return s.cache_items + (seen + s.item_keys - 1) / s.item_keys;
 }
 
 // Tile size.  Where all rows of a stream fill at most half or a quarter of a tile, the tile holds them two or four times, and each copy takes
@@ -68,8 +67,8 @@ __host__ __device__
 #endif
 inline bool chunk_needs_slot(const ChunkShape& s, int begin, int end, int items) { return s.copies > 1 || begin > 0 || end < items; }
 
-// Returns the number of slots, or 0 with cuts->n = 0 where there is nothing to do.
-inline int chunk_plan(const ChunkShape& s, const int32_t* len, ChunkCuts* cuts, ChunkMerge* merge) {
+// min_items: what a CTA is worth starting for.  Returns the number of slots, or 0 with cuts->n = 0 where there is nothing to do.
+inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, ChunkCuts* cuts, ChunkMerge* merge) {
   int64_t total = 0;
   for (int b = 0; b < s.batch; ++b) {
     const int n = chunk_len(s, len, b);
@@ -79,7 +78,7 @@ inline int chunk_plan(const ChunkShape& s, const int32_t* len, ChunkCuts* cuts, 
   merge->n = 0;
   merge->slot[0] = 0;
   if (total == 0) return 0;
-  const int n_ctas = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / kChunkMinItems)));
+  const int n_ctas = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / min_items)));
   // tiles in the order (sequence, KV head, row tile)
   int64_t at = 0;
   int c = 0, slots = 0, tile = 0;
@@ -127,11 +126,42 @@ struct ChunkCall {
   uint16_t* out;
   float *lse, *workspace;
   uint32_t* status;
-  int32_t table_stride;
+  int32_t table_stride, n_closed, n_tail, res_rows;      // residual rows: of the stream that has most
   float scale;
   ChunkShape shape;
 };
+template <int N>
+struct ChunkLens {                          // N = 1: every sequence has n_new rows
+  int32_t len[N];
+};
 cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
+cudaError_t launch_verify(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
+cudaError_t launch_chunk_merge(const ChunkCall& call, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
 #endif
+
+// A step coprime to n, about 0.618 of it: multiplied by it, neighbouring places of a walk are blocks of different ages.
+inline int chunk_walk(int n) {
+  if (n <= 2) return 1;
+  auto gcd = [](int a, int b) {
+    while (b) {
+      const int t = a % b;
+      a = b;
+      b = t;
+    }
+    return a;
+  };
+  int walk = static_cast<int>(n * 0.6180339887);
+  while (gcd(walk, n) != 1) ++walk;
+  return walk;
+}
+
+// ---- chunks of few rows (gkv_verify.cu): a tile is a stream, an item half a block, 32 keys ----
+constexpr int kVerifyRows = 64;
+inline void verify_shape(ChunkShape* s, int n_closed, int n_tail, int res_rows) {
+  s->tile_tokens = s->n_new;
+  s->row_tiles = s->copies = 1;
+  s->item_keys = 32;
+  s->cache_items = 2 * n_closed + (n_tail + 31) / 32 + (res_rows + 31) / 32;
+}
 
 }  // namespace gkv

@@ -10,15 +10,16 @@ from paper_2608_23599_b200 import build as _build
 
 HARNESS = r"""
 #include <cstdio>
+#include <numeric>
 #include <random>
 #include <vector>
 #include "gkv_chunk.h"
 using namespace gkv;
 
-static int check(const ChunkShape& s, const int32_t* len) {
+static int check(const ChunkShape& s, const int32_t* len, int min_items) {
   ChunkCuts cuts;
   ChunkMerge merge;
-  const int slots = chunk_plan(s, len, &cuts, &merge);
+  const int slots = chunk_plan(s, len, min_items, &cuts, &merge);
   const int tiles = s.batch * s.n_kv_heads * s.row_tiles;
   if (s.tile_tokens * s.group * s.copies > kChunkRows || s.tile_tokens < 1 || s.row_tiles * s.tile_tokens < s.n_new) return 1;
   long total = 0;
@@ -69,15 +70,17 @@ int main() {
     s.n_kv_heads = 1 + upto(8);
     s.group = 1 + upto(7);
     s.n_new = 1 + upto(i % 3 == 0 ? 700 : 20);
-    s.n_closed = upto(i % 5 == 0 ? 600 : 12);
-    s.n_tail = upto(63);
-    s.res_groups = upto(3);
+    const int n_closed = upto(i % 5 == 0 ? 600 : 12), n_tail = upto(63), res_rows = upto(3) * 50;
     chunk_shape(&s);
+    s.item_keys = 64;
+    s.cache_items = n_closed + (n_tail > 0) + (res_rows + 63) / 64;
+    if (s.n_new * s.group <= kVerifyRows && upto(1)) verify_shape(&s, n_closed, n_tail, res_rows);
+    if (std::gcd(chunk_walk(n_closed + 1), n_closed + 1) != 1) return 2;
     std::vector<int32_t> len(s.batch);
     for (auto& n : len) n = upto(3) ? upto(s.n_new) : 0;
     for (const int32_t* l : {static_cast<const int32_t*>(nullptr), static_cast<const int32_t*>(len.data())})
-      if (const int rc = check(s, l)) {
-        std::printf("case %d: %d (batch %d kv %d group %d new %d closed %d)\n", i, rc, s.batch, s.n_kv_heads, s.group, s.n_new, s.n_closed);
+      if (const int rc = check(s, l, 1 + upto(8))) {
+        std::printf("case %d: %d (batch %d kv %d group %d new %d closed %d)\n", i, rc, s.batch, s.n_kv_heads, s.group, s.n_new, n_closed);
         return 1;
       }
   }
