@@ -13,7 +13,8 @@
 // any number of rows and every value written to shared memory first: with up to 64 rows a kernel of that kind took 1.9 times as long.
 //
 // Work split.  gkv_chunk.h cuts the streams' items (half blocks: 32 tokens) into equal ranges, one per CTA.  The CTA's warps form teams of
-// one warp per 16 rows; a team takes every n-th item of the range and streams it through a ring of its own, filled by its first warp with bulk copies.
+// one warp per 16 rows; a team takes every n-th item of the range and streams it through a ring of its own.  The rings are filled with bulk copies by
+// one warp more, a lane per team.  (The team's first warp needed 1400 cycles of 6100 per half block for that.)
 // The teams' results are merged in shared memory in team order, the CTAs' by chunk_merge_kernel.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -28,8 +29,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int kVWarps = 12;                // 168 registers a thread
-constexpr int kVThreads = kVWarps * 32;
+constexpr int kVWarps = 12;                // that compute
+constexpr int kVThreads = kVWarps * 32 + 128;
+constexpr int kVLaunchRegs = 128, kVWarpRegs = 152, kVFillRegs = 56;
+static_assert(kVWarps / 4 * kVWarpRegs + kVFillRegs <= (kVWarps / 4 + 1) * kVLaunchRegs, "a split draws on the launch's registers");
 constexpr int kVStage = 5120;              // a 4-bit half block, the keys or the values of an 8-bit one, or of 16 exact rows
 constexpr int kVPitch = kRowBytes + 16;    // exact rows (conflict-free ldmatrix)
 constexpr int kVMeta = 96;                 // a stage's description
@@ -137,6 +140,18 @@ __device__ __forceinline__ uint32_t code_bits(const uint32_t (&w)[4], int i, int
 }
 __device__ __forceinline__ constexpr int code_exp(int bits, int y) { return y == 0 || bits == 8 ? 0 : bits == 4 ? 4 : 2; }
 
+// q s as an fp16 pair: the rounded product and what is left of it (exact)
+__device__ __forceinline__ void split(uint32_t q, uint32_t s, uint32_t& hi, uint32_t& lo) {
+  asm("{\n"
+      ".reg .b32 n;\n"
+      "mul.rn.f16x2 %0, %2, %3;\n"
+      "neg.f16x2 n, %0;\n"
+      "fma.rn.f16x2 %1, %2, %3, n;\n"
+      "}\n"
+      : "=&r"(hi), "=r"(lo)
+      : "r"(q), "r"(s));
+}
+
 struct VState {
   float o[16][4], oz[4];     // channels 8 n + 2 c4, + 1 of rows r (0, 1) and r + 8 (2, 3); groups 2 c4, + 1
   float m0, m1, l0, l1;      // references of the two rows (units of q . k), this lane's part of their sums
@@ -205,21 +220,17 @@ __device__ __forceinline__ void code_logits(float (&x)[4][4], uint32_t raw, uint
       const uint4 qv = lds128(q + ((2 * j + i) * 32 + lane) * 16);
       const uint32_t a[4] = {qv.x, qv.y, qv.z, qv.w};
       mma_f16(z, a, pick(zr, i), pick(zr, 2 + i));
-      uint32_t hi[4], lo[4];
+      uint32_t hi[4], lo[4], b[4][2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const __half2 s = h2(pick(sr, (k >> 1) * 2 + i)), h = __hmul2(h2(a[k]), s);
-        hi[k] = u32(h);
-        lo[k] = u32(__hfma2(h2(a[k]), s, __hneg2(h)));
+      for (int k = 0; k < 4; ++k) split(a[k], pick(sr, (k >> 1) * 2 + i), hi[k], lo[k]);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {          // (a tile's two products are apart: the second waits for the first's sum)
+        b[n][0] = code_bits<BITS, false>(w[n >> 1], i, n & 1);
+        b[n][1] = code_bits<BITS, false>(w[n >> 1], i, (n & 1) + 2);
+        mma_f16(x[n], hi, b[n][0], b[n][1]);
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const uint32_t b0 = code_bits<BITS, false>(w[t], i, y), b1 = code_bits<BITS, false>(w[t], i, y + 2);
-          mma_f16(x[2 * t + y], hi, b0, b1);
-          mma_f16(x[2 * t + y], lo, b0, b1);
-        }
+      for (int n = 0; n < 4; ++n) mma_f16(x[n], lo, b[n][0], b[n][1]);
     }
   }
 #pragma unroll
@@ -275,17 +286,60 @@ struct VerifyParams {
   ChunkShape s;
 };
 
-// A team's walk over its items, in the lanes of its first warp.
-struct VWalk {
-  int it, end, step;         // items
-  int base;                  // first item of the window
-  uint32_t off, level;       // this lane's entry: item base + lane * step
-  uint64_t res;
-  int pend;                  // centroids collected
-  // the rest of a row item
-  uint64_t k, v;
-  uint32_t stride, hide;
-  int rows, causal;
+// What one lane does for its team: walks the team's items and fills its ring.
+struct VFill {
+  uint32_t ring, bar_full, bar_free;
+  VMeta* meta;
+  int places, at;
+  uint32_t turn;             // parity of the place's last turn (places that have not been used yet count as freed)
+  volatile uint32_t* abort;
+  // one part; the entry and its bytes
+  __device__ __forceinline__ bool begin(int kind, int level, int n, int causal, uint32_t hide, uint32_t bytes, const float* bias = nullptr) {
+    if (!bar_wait(bar_free + 8 * at, turn, abort)) return false;
+    VMeta& e = meta[at];
+    e.kind = kind;
+    e.level = level;
+    e.n = n;
+    e.causal = causal;
+    e.hide = hide;
+    if (bias)
+      for (int i = 0; i < 16; ++i) e.bias[i] = bias[i < n ? i : 0];
+    if (bytes) bar_expect(bar_full + 8 * at, bytes);
+    return true;
+  }
+  __device__ __forceinline__ void next() {
+    if (++at == places) {
+      at = 0;
+      turn ^= 1u;
+    }
+  }
+  __device__ __forceinline__ bool piece(const uint8_t* src, uint32_t bytes, int kind, int level, uint32_t hide) {
+    if (!begin(kind, level, 0, -1, hide, bytes)) return false;
+    bulk_load(ring + at * kVStage, src, bytes, bar_full + 8 * at);
+    next();
+    return true;
+  }
+  // 16 rows (those that are not there: the first one again, their keys are masked)
+  __device__ __forceinline__ bool rows(const uint8_t* src, uint32_t stride, int n, int causal, uint32_t hide) {
+    if (!begin(2, 16, n, causal, hide, 16 * kRowBytes)) return false;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) bulk_load(ring + at * kVStage + i * kVPitch, src + (i < n ? static_cast<size_t>(i) * stride : 0), kRowBytes, bar_full + 8 * at);
+    next();
+    return true;
+  }
+  __device__ __forceinline__ bool centroids(const uint8_t* arena, const uint32_t* off, const float* bias, int n) {
+    if (!begin(3, 1, n, -1, 0, 16 * kRowBytes, bias)) return false;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) bulk_load(ring + at * kVStage + i * kVPitch, arena + static_cast<size_t>(off[i < n ? i : 0]) * 256, kRowBytes, bar_full + 8 * at);
+    next();
+    return true;
+  }
+  __device__ __forceinline__ bool end() {
+    if (!begin(0, 0, 0, -1, 0, 0)) return false;
+    bar_arrive(bar_full + 8 * at);
+    next();
+    return true;
+  }
 };
 
 template <int N>
@@ -295,18 +349,18 @@ __global__ void __launch_bounds__(kVThreads, 1)
   const uint32_t smem = smem_u32(smem_raw);
   const VLayout lay = verify_layout(p.groups);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c4 = lane & 3;
-  const int team = warp / p.groups, grp = warp % p.groups;
-  const bool in_team = team < lay.teams;
+  const bool fills = warp == kVWarps && lane < lay.teams;                 // (the other warps of its four have nothing to do)
+  const int team = warp < kVWarps ? warp / p.groups : lane, grp = warp < kVWarps ? warp % p.groups : 0;
+  const bool in_team = warp < kVWarps && team < lay.teams;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(smem_raw + lay.bars + lay.teams * lay.ring * 16);
   const ChunkShape& sh = p.s;
   const float c = p.scale_log2;
-  const uint32_t ring = smem + lay.stages + (in_team ? team : 0) * lay.ring * kVStage;
-  const uint32_t bar_full = smem + lay.bars + (in_team ? team : 0) * lay.ring * 16, bar_free = bar_full + 8 * lay.ring;
-  VMeta* const meta = reinterpret_cast<VMeta*>(smem_raw + lay.meta) + (in_team ? team : 0) * lay.ring;
-  uint32_t* const pend_off = reinterpret_cast<uint32_t*>(smem_raw + lay.pend) + (in_team ? team : 0) * kVPend * 2;
-  float* const pend_bias = reinterpret_cast<float*>(pend_off + kVPend);
+  const int mine = in_team || fills ? team : 0;
+  const uint32_t ring = smem + lay.stages + mine * lay.ring * kVStage;
+  const uint32_t bar_full = smem + lay.bars + mine * lay.ring * 16, bar_free = bar_full + 8 * lay.ring;
+  VMeta* const meta = reinterpret_cast<VMeta*>(smem_raw + lay.meta) + mine * lay.ring;
   if (threadIdx.x == 0) *abort = 0;
-  if (in_team && grp == 0 && lane == 0) {
+  if (fills) {
     for (int i = 0; i < lay.ring; ++i) {
       bar_init(bar_full + 8 * i, 1);
       bar_init(bar_free + 8 * i, p.groups);
@@ -315,34 +369,124 @@ __global__ void __launch_bounds__(kVThreads, 1)
   }
   const int cta = blockIdx.x, t0 = cuts.tile[cta], i0 = cuts.item[cta], t1 = cuts.tile[cta + 1], i1 = cuts.item[cta + 1];
   int slot = cuts.slot[cta];
-  int put = 0, got = 0;                    // parts of the ring that the team's first warp has filled, that this warp has used
+  int got_at = 0;                          // place of the ring, and its turn's parity
+  uint32_t got_turn = 0;
   bool ok = true;
-
-  for (int tile = t0; tile <= t1 && tile < sh.batch * sh.n_kv_heads; ++tile) {
-    const int b = tile / sh.n_kv_heads, h = tile % sh.n_kv_heads;
-    const int len = lens.len[N == 1 ? 0 : b];
-    const int items = chunk_items(sh, len, 0);
-    const int begin = tile == t0 ? i0 : 0, end = tile == t1 ? i1 : items;
-    if (begin >= end) continue;
-    const int rows = len * sh.group;
-    __syncthreads();                       // (barriers are initialised; the previous stream's merge has been read)
-    // the rows' fragments: lane (r, c4) of MMA index s holds channels 16 s + 2 c4, + 1 of rows r and r + 8, then the channels eight further
-    for (int i = threadIdx.x; i < p.groups * 8 * 32; i += kVThreads) {
-      const int s = i >> 5 & 7, g16 = i >> 8, ln = i & 31;
-      uint32_t x[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int row = g16 * 16 + (ln >> 2) + 8 * (k & 1), ch = 16 * s + 2 * (ln & 3) + 8 * (k >> 1);
-        uint32_t u = 0;
-        if (row < rows)
-          u = *reinterpret_cast<const uint32_t*>(
-              p.q + ((static_cast<size_t>(b) * sh.n_new + row / sh.group) * (sh.n_kv_heads * sh.group) + h * sh.group + row % sh.group) * kD + ch);
-        x[k] = f16_pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
-      }
-      sts128(smem + lay.q + i * 16, make_uint4(x[0], x[1], x[2], x[3]));
+  // Both branches walk the same streams of the CTA's range and meet at the same barriers.
+  struct Part {
+    int tile, b, h, len, items, begin, end;
+  };
+  auto next_part = [&](int from, Part& x) {
+    for (x.tile = from; x.tile <= t1 && x.tile < sh.batch * sh.n_kv_heads; ++x.tile) {
+      x.b = x.tile / sh.n_kv_heads;
+      x.h = x.tile % sh.n_kv_heads;
+      x.len = lens.len[N == 1 ? 0 : x.b];
+      x.items = chunk_items(sh, x.len, 0);
+      x.begin = x.tile == t0 ? i0 : 0;
+      x.end = x.tile == t1 ? i1 : x.items;
+      if (x.begin < x.end) return true;
     }
-    fence_async();                         // (the merge wrote where copies land next)
+    return false;
+  };
+  Part x;
+
+  if (warp >= kVWarps) {
+    fewer_regs<kVFillRegs>();
+    VFill fill{ring, bar_full, bar_free, meta, lay.ring, 0, 1u, abort};
+    for (int from = t0; next_part(from, x); from = x.tile + 1) {
+    const int tile = x.tile, b = x.b, h = x.h, len = x.len, begin = x.begin, end = x.end;
+    __syncthreads();                       // (barriers are initialised; the previous stream's merge has been read)
+    if (fills) {
+      // ---- the walk of one team ----
+      const TableEntry* table = p.table + static_cast<size_t>(tile) * p.table_stride;
+      const int blocks_end = 2 * p.n_closed, tail_end = blocks_end + (p.n_tail + 31) / 32, res_end = tail_end + p.res_items;
+      uint32_t* const pend_off = reinterpret_cast<uint32_t*>(smem_raw + lay.pend) + team * kVPend * 2;
+      float* const pend_bias = reinterpret_cast<float*>(pend_off + kVPend);
+      int pend = 0;
+      auto entry = [&](int it) {           // of an item's block
+        return it < min(end, blocks_end) ? *reinterpret_cast<const uint4*>(
+                                               table + static_cast<uint64_t>(it >> 1) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(p.n_closed))
+                                         : make_uint4(0, 0, 0, 0);
+      };
+      auto row_item = [&](const uint8_t* k, const uint8_t* v, uint32_t stride, int n, int causal, uint32_t hide) {
+        for (int i = 0; ok && i < n; i += 16) {
+          const size_t at = static_cast<size_t>(i) * stride;
+          const int take = min(16, n - i), from = causal < 0 ? -1 : causal + i;
+          ok = fill.rows(k + at, stride, take, from, hide >> i & 0xffffu) && fill.rows(v + at, stride, take, from, 0);
+        }
+      };
+      uint4 e = entry(begin + team);
+      for (int it = begin + team; ok && it < end; it += lay.teams) {
+        if (it < blocks_end) {
+          const uint4 now = e;
+          e = entry(it + lay.teams);
+          const int half = it & 1, level = static_cast<int>(now.y);
+          const uint8_t* at = p.arena + static_cast<size_t>(now.x) * 256;
+          if (level == 1) {
+            if (half) continue;
+            const int n = kBlock - __popc(now.z) - __popc(now.w);
+            pend_off[pend] = now.x;
+            pend_bias[pend] = n > 0 ? lg2(static_cast<float>(n)) / c : -INFINITY;
+            if (++pend == 16) {
+              ok = fill.centroids(p.arena, pend_off, pend_bias, 16) && fill.centroids(p.arena + kRowBytes, pend_off, pend_bias, 16);
+              pend = 0;
+            }
+          } else if (level == 16) {
+            const uint8_t* k = at + half * 32 * kRowBytes;
+            row_item(k, k + kBlock * kRowBytes, kRowBytes, 32, -1, half ? now.w : now.z);
+          } else {
+            const uint32_t bytes = half_bytes(level), hide = half ? now.w : now.z;
+            if (level == 8)
+              ok = fill.piece(at + half * bytes, bytes / 2, 1, 8, hide) && fill.piece(at + half * bytes + bytes / 2, bytes / 2, 1, 8, 0);
+            else ok = fill.piece(at + half * bytes, bytes, 1, level, hide);
+          }
+        } else if (it < tail_end) {
+          const int row0 = (it - blocks_end) * 32;
+          const uint8_t* k = p.arena + static_cast<size_t>(table[p.n_closed].off256) * 256 + row0 * kRowBytes;
+          row_item(k, k + kBlock * kRowBytes, kRowBytes, min(32, p.n_tail - row0), -1, 0);
+        } else if (it < res_end) {
+          const int row0 = (it - tail_end) * 32;
+          const uint8_t* k = p.arena + static_cast<size_t>(p.res_off256[tile]) * 256 + static_cast<size_t>(row0) * 2 * kRowBytes;
+          row_item(k, k + kRowBytes, 2 * kRowBytes, min(32, p.res_count[tile] - row0), -1, 0);
+        } else {
+          const int tok0 = (it - res_end) * 32;
+          const size_t at = ((static_cast<size_t>(b) * sh.n_new + tok0) * sh.n_kv_heads + h) * kRowBytes;
+          row_item(reinterpret_cast<const uint8_t*>(p.k_new) + at, reinterpret_cast<const uint8_t*>(p.v_new) + at, static_cast<uint32_t>(sh.n_kv_heads) * kRowBytes,
+                   min(32, len - tok0), tok0, 0);
+        }
+      }
+      if (ok && pend > 0) ok = fill.centroids(p.arena, pend_off, pend_bias, pend) && fill.centroids(p.arena + kRowBytes, pend_off, pend_bias, pend);
+      ok = ok && fill.end();
+      if (!ok)                             // what is on its way arrives before the memory is used otherwise
+        for (int i = 0; i < lay.ring; ++i) bar_drain(bar_full + 8 * i, i < fill.at ? fill.turn ^ 1u : fill.turn);
+    }
+    __syncwarp();
     __syncthreads();
+    __syncthreads();
+    if (*abort) break;
+    }
+  } else {
+    more_regs<kVWarpRegs>();
+    for (int from = t0; next_part(from, x); from = x.tile + 1) {
+    const int b = x.b, h = x.h, len = x.len, items = x.items, begin = x.begin, end = x.end;
+    const int rows = len * sh.group;
+    __syncthreads();
+    // the rows' fragments: lane (r, c4) of MMA index s holds channels 16 s + 2 c4, + 1 of rows r and r + 8, then the channels eight further
+      for (int i = threadIdx.x; i < p.groups * 8 * 32; i += kVWarps * 32) {
+        const int s = i >> 5 & 7, g16 = i >> 8, ln = i & 31;
+        uint32_t x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int row = g16 * 16 + (ln >> 2) + 8 * (k & 1), ch = 16 * s + 2 * (ln & 3) + 8 * (k >> 1);
+          uint32_t u = 0;
+          if (row < rows)
+            u = *reinterpret_cast<const uint32_t*>(
+                p.q + ((static_cast<size_t>(b) * sh.n_new + row / sh.group) * (sh.n_kv_heads * sh.group) + h * sh.group + row % sh.group) * kD + ch);
+          x[k] = f16_pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+        }
+        sts128(smem + lay.q + i * 16, make_uint4(x[0], x[1], x[2], x[3]));
+      }
+    asm volatile("bar.sync 1, %0;\n" ::"n"(kVWarps * 32) : "memory");
 
     VState st;
 #pragma unroll
@@ -352,191 +496,23 @@ __global__ void __launch_bounds__(kVThreads, 1)
     st.l0 = st.l1 = 0.f;
 
     if (in_team) {
-      const TableEntry* table = p.table + static_cast<size_t>(tile) * p.table_stride;
-      const int blocks_end = 2 * p.n_closed, tail_end = blocks_end + (p.n_tail + 31) / 32, res_end = tail_end + p.res_items;
-      VWalk wk{};
-      wk.it = begin + team;
-      wk.end = end;
-      wk.step = lay.teams;
-      wk.base = -1;
-      bool more = true;                    // the walk has not ended
-
-      // Fills a part of the ring; whole first warps.  Row parts: lane i < 16 copies row i (rows that are not there: row 0 again, their keys are masked)
-      auto part = [&](const VMeta& m, uint64_t src, uint32_t bytes, uint64_t row, bool by_row) {
-        const int at = put % lay.ring;
-        if (put >= lay.ring) ok = ok && bar_wait(bar_free + 8 * at, (put / lay.ring - 1) & 1, abort);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return;
-        VMeta& e = meta[at];
-        if (lane == 0) {
-          e.kind = m.kind;
-          e.level = m.level;
-          e.n = m.n;
-          e.causal = m.causal;
-          e.hide = m.hide;
-        }
-        if (m.kind == 3 && lane < 16) e.bias[lane] = m.bias[0];
-        __syncwarp();
-        const uint32_t dst = ring + at * kVStage, bar = bar_full + 8 * at;
-        if (lane == 0) {
-          if (bytes) bar_expect(bar, by_row ? 16 * kRowBytes : bytes);
-          else bar_arrive(bar);
-        }
-        __syncwarp();
-        if (by_row) {
-          if (lane < 16) bulk_load(dst + lane * kVPitch, reinterpret_cast<const void*>(row), kRowBytes, bar);
-        } else if (bytes && lane == 0) {
-          bulk_load(dst, reinterpret_cast<const void*>(src), bytes, bar);
-        }
-        ++put;
-      };
-      // The next step of the walk goes into the ring (one part or two); false at its end.
-      auto produce = [&]() {
-        VMeta m{};
-        m.causal = -1;
-        for (;;) {
-          if (wk.rows > 0) {               // 16 rows of a row item
-            m.kind = 2;
-            m.n = min(wk.rows, 16);
-            m.hide = wk.hide & 0xffffu;
-            m.causal = wk.causal;
-            const int i = lane < m.n ? lane : 0;
-            part(m, 0, 1, wk.k + static_cast<uint64_t>(i) * wk.stride, true);
-            part(m, 0, 1, wk.v + static_cast<uint64_t>(i) * wk.stride, true);
-            wk.rows -= m.n;
-            wk.hide >>= 16;
-            wk.k += static_cast<uint64_t>(16) * wk.stride;
-            wk.v += static_cast<uint64_t>(16) * wk.stride;
-            if (wk.causal >= 0) wk.causal += 16;
-            return;
-          }
-          if (wk.pend >= 16 || (wk.it >= wk.end && wk.pend > 0)) {
-            m.kind = 3;
-            m.n = min(wk.pend, 16);
-            const int i = lane < m.n ? lane : 0;
-            const uint64_t row = reinterpret_cast<uint64_t>(p.arena) + static_cast<uint64_t>(pend_off[i]) * 256;
-            m.bias[0] = pend_bias[i];
-            part(m, 0, 1, row, true);
-            part(m, 0, 1, row + kRowBytes, true);
-            __syncwarp();
-            uint32_t o = 0;
-            float f = 0.f;
-            const int left = wk.pend - m.n;      // at most 47
-            for (int k = 0; k < left; k += 32) {
-              if (k + lane < left) {
-                o = pend_off[16 + k + lane];
-                f = pend_bias[16 + k + lane];
-              }
-              __syncwarp();
-              if (k + lane < left) {
-                pend_off[k + lane] = o;
-                pend_bias[k + lane] = f;
-              }
-              __syncwarp();
-            }
-            wk.pend = left;
-            return;
-          }
-          if (wk.it >= wk.end) {
-            more = false;
-            part(m, 0, 0, 0, false);       // "no more"
-            return;
-          }
-          const int it = wk.it;
-          if (it < blocks_end) {
-            if (wk.base < 0 || it >= wk.base + 32 * wk.step) {
-              const int mine = it + lane * wk.step;
-              wk.base = it;
-              uint4 e = make_uint4(0, 0, 0, 0);
-              if (mine < min(wk.end, blocks_end))
-                e = *reinterpret_cast<const uint4*>(table + static_cast<uint64_t>(mine >> 1) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(p.n_closed));
-              wk.off = e.x;
-              wk.level = e.y;
-              wk.res = static_cast<uint64_t>(e.w) << 32 | e.z;
-              const bool cent = wk.level == 1 && !(mine & 1);
-              const uint32_t cents = __ballot_sync(0xffffffffu, cent);
-              if (cent) {
-                const int at = wk.pend + __popc(cents & ((1u << lane) - 1u)), n = kBlock - __popcll(wk.res);
-                pend_off[at] = wk.off;
-                pend_bias[at] = n > 0 ? lg2(static_cast<float>(n)) / c : -INFINITY;
-              }
-              __syncwarp();
-              wk.pend += __popc(cents);
-              if (wk.pend >= 16) continue;
-            }
-            const int from = (it - wk.base) / wk.step;
-            const uint32_t off = __shfl_sync(0xffffffffu, wk.off, from);
-            const int level = static_cast<int>(__shfl_sync(0xffffffffu, wk.level, from));
-            const uint64_t res = __shfl_sync(0xffffffffu, wk.res, from);
-            wk.it += wk.step;
-            if (level == 1) continue;
-            const int half = it & 1;
-            const uint64_t at = reinterpret_cast<uint64_t>(p.arena) + static_cast<uint64_t>(off) * 256;
-            const uint32_t hide = static_cast<uint32_t>(half ? res >> 32 : res);
-            if (level == 16) {
-              wk.rows = 32;
-              wk.hide = hide;
-              wk.causal = -1;
-              wk.stride = kRowBytes;
-              wk.k = at + half * 32 * kRowBytes;
-              wk.v = wk.k + kBlock * kRowBytes;
-              continue;
-            }
-            m.kind = 1;
-            m.level = level;
-            m.hide = hide;
-            const uint32_t bytes = half_bytes(level);
-            if (level == 8) {
-              part(m, at + half * bytes, bytes / 2, 0, false);
-              part(m, at + half * bytes + bytes / 2, bytes / 2, 0, false);
-            } else {
-              part(m, at + half * bytes, bytes, 0, false);
-            }
-            return;
-          }
-          wk.it += wk.step;
-          wk.hide = 0;
-          wk.causal = -1;
-          if (it < tail_end) {
-            const int row0 = (it - blocks_end) * 32;
-            wk.rows = min(32, p.n_tail - row0);
-            wk.stride = kRowBytes;
-            wk.k = reinterpret_cast<uint64_t>(p.arena) + static_cast<uint64_t>(table[p.n_closed].off256) * 256 + row0 * kRowBytes;
-            wk.v = wk.k + kBlock * kRowBytes;
-          } else if (it < res_end) {
-            const int row0 = (it - tail_end) * 32;
-            wk.rows = max(0, min(32, p.res_count[tile] - row0));
-            wk.stride = 2 * kRowBytes;
-            wk.k = reinterpret_cast<uint64_t>(p.arena) + static_cast<uint64_t>(p.res_off256[tile]) * 256 + static_cast<uint64_t>(row0) * 2 * kRowBytes;
-            wk.v = wk.k + kRowBytes;
-          } else {
-            const int tok0 = (it - res_end) * 32;
-            const size_t at = (static_cast<size_t>(b) * sh.n_new + tok0) * sh.n_kv_heads + h;
-            wk.rows = min(32, len - tok0);
-            wk.causal = tok0;
-            wk.stride = static_cast<uint32_t>(sh.n_kv_heads) * kRowBytes;
-            wk.k = reinterpret_cast<uint64_t>(p.k_new + at * kD);
-            wk.v = reinterpret_cast<uint64_t>(p.v_new + at * kD);
-          }
-        }
-      };
-      auto wait_part = [&]() { return bar_wait(bar_full + 8 * (got % lay.ring), (got / lay.ring) & 1, abort); };
+      auto wait_part = [&]() { return bar_wait(bar_full + 8 * got_at, got_turn, abort); };
       auto free_part = [&]() {
         __syncwarp();
-        if (lane == 0) bar_arrive(bar_free + 8 * (got % lay.ring));
-        ++got;
+        if (lane == 0) bar_arrive(bar_free + 8 * got_at);
+        if (++got_at == lay.ring) {
+          got_at = 0;
+          got_turn ^= 1u;
+        }
       };
 
       const int row0 = grp * 16 + r, tok_a = row0 / sh.group, tok_b = (row0 + 8) / sh.group;      // of the lane's two rows
       const uint32_t q = smem + lay.q + grp * 4096;
       for (;;) {
-        // as many steps ahead as the ring holds for certain (a step has one part or two)
-        if (grp == 0)
-          while (ok && more && put - got + 2 <= lay.ring) produce();
-        if (!ok || !(ok = wait_part())) break;
-        const VMeta& e = meta[got % lay.ring];
+        if (!(ok = wait_part())) break;
+        const VMeta& e = meta[got_at];
         const int kind = e.kind, level = e.level;
-        const uint32_t raw = ring + (got % lay.ring) * kVStage;
+        const uint32_t raw = ring + got_at * kVStage;
         if (kind == 0) {
           free_part();
           break;
@@ -558,7 +534,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
           if (level == 8) {
             free_part();
             if (!(ok = wait_part())) break;
-            code_values<8>(st, x, ring + (got % lay.ring) * kVStage - half_bytes(8) / 2, lane);
+            code_values<8>(st, x, ring + got_at * kVStage - half_bytes(8) / 2, lane);
           } else if (level == 4) {
             code_values<4>(st, x, raw, lane);
           } else {
@@ -606,7 +582,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
           const float down = 1.f / kVUp;
           const uint32_t a[4] = {bf16_pair(x[0][0] * down, x[0][1] * down), bf16_pair(x[0][2] * down, x[0][3] * down), bf16_pair(x[1][0] * down, x[1][1] * down),
                                  bf16_pair(x[1][2] * down, x[1][3] * down)};
-          const uint32_t vm = ring + (got % lay.ring) * kVStage + (lane & 15) * kVPitch + (lane >> 4) * 16;
+          const uint32_t vm = ring + got_at * kVStage + (lane & 15) * kVPitch + (lane >> 4) * 16;
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
             uint32_t vb[4];
@@ -616,9 +592,6 @@ __global__ void __launch_bounds__(kVThreads, 1)
           }
           free_part();
         }
-      }
-      if (!ok && grp == 0) {                 // what is on its way arrives before the memory is used otherwise
-        for (int i = max(0, put - lay.ring); i < put; ++i) bar_drain(bar_full + 8 * (i % lay.ring), (i / lay.ring) & 1);
       }
       // the four lanes of a row hold its sum in parts; zero points of group n / 4 come from the lane that has its column
 #pragma unroll
@@ -655,28 +628,30 @@ __global__ void __launch_bounds__(kVThreads, 1)
         mml[warp * 16 + r + 8] = make_float2(st.m1 * c, st.l1);
       }
     }
+    fence_async();                         // (copies land there next)
     __syncthreads();
     const int to = chunk_needs_slot(sh, begin, end, items) ? slot++ : -1;
-    for (int i = warp; i < rows; i += kVWarps) {           // a warp per row, four channels per lane
-      const int g16 = i >> 4, in = i & 15;
-      float top = -INFINITY;
-      for (int t = 0; t < lay.teams; ++t) {
-        const float2 v = mml[(t * p.groups + g16) * 16 + in];
-        if (v.y > 0.f) top = fmaxf(top, v.x);
-      }
-      float sum = 0.f;
+    for (int i = warp; i < rows; i += kVWarps) {           // a warp per row, four channels per lane; lane t has team t's factor
+      const int at0 = (i >> 4) * 16 + (i & 15), step = p.groups * 16;
+      const float2 v = lane < lay.teams ? mml[at0 + lane * step] : make_float2(0.f, 0.f);
+      float top = v.y > 0.f ? v.x : -INFINITY;
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));      // (at most 12 teams)
+      const float f = v.y > 0.f ? ex2(v.x - top) : 0.f;
+      float sum = f * v.y;
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      top = __shfl_sync(0xffffffffu, top, 0);
+      sum = __shfl_sync(0xffffffffu, sum, 0);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
       for (int t = 0; t < lay.teams; ++t) {
-        const int at = (t * p.groups + g16) * 16 + in;
-        const float2 v = mml[at];
-        if (!(v.y > 0.f)) continue;
-        const float f = ex2(v.x - top);
-        const float4 x = *reinterpret_cast<const float4*>(mo + at * kVOPitch + 4 * lane);
-        sum += f * v.y;
-        o.x += f * x.x;
-        o.y += f * x.y;
-        o.z += f * x.z;
-        o.w += f * x.w;
+        const float g = __shfl_sync(0xffffffffu, f, t);
+        const float4 x = *reinterpret_cast<const float4*>(mo + (at0 + t * step) * kVOPitch + 4 * lane);
+        o.x += g * x.x;
+        o.y += g * x.y;
+        o.z += g * x.z;
+        o.w += g * x.w;
       }
       if (to >= 0) {
         const size_t at = static_cast<size_t>(to) * kChunkRows + i;
@@ -691,6 +666,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
     }
     if (!ok) atomicOr(p.status, kStatusInternal);
     if (*abort) break;                       // (set by whoever gave up: everyone has passed the barrier behind its waits)
+    }
   }
 }
 
