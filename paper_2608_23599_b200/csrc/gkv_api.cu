@@ -2008,6 +2008,7 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
   const int slots = chunk_plan(call.shape, len, few ? 6 : 4, &cuts, &merge);
   if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
   call.arena = c->arena;
+  call.arena_bytes = c->arena_bytes;
   call.table = L.table_d;
   call.table_stride = c->table_stride;
   call.res_off256 = L.res_off_d;

@@ -119,6 +119,7 @@ inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, Ch
 struct TableEntry;
 struct ChunkCall {
   const uint8_t* arena;
+  size_t arena_bytes;
   const TableEntry* table;
   const uint32_t* res_off256;
   const int32_t* res_count;

@@ -533,6 +533,13 @@ int check_prompt(const gkv_prompt* d, int* rows) {
   return GKV_OK;
 }
 
+// A map of [rows][heads][128] 16-bit elements: boxes of 64 channels x `heads_box` heads x `rows_box` rows.  Rows are `stride` elements apart.
+bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int heads, int64_t stride, int heads_box, int rows_box) {
+  const uint64_t dims[3] = {kD, static_cast<uint64_t>(heads), static_cast<uint64_t>(rows)}, strides[2] = {kD * 2, static_cast<uint64_t>(stride) * 2};
+  const uint32_t box[3] = {64, static_cast<uint32_t>(heads_box), static_cast<uint32_t>(rows_box)};
+  return make_map(map, base, 3, dims, strides, box);
+}
+
 // Sequences [begin, end) with rows, longest first, `per` tokens to a work item.
 template <int N>
 int deal(Seqs<N>& s, const int32_t* offsets, const std::vector<int>& order, int begin, int end, int per) {
@@ -598,9 +605,8 @@ bool on_current_device(std::initializer_list<const void*> ptrs) {
   return true;
 }
 
-// A map of [rows][heads][128] 16-bit elements: boxes of 64 channels x `heads_box` heads x `rows_box` rows, 128-byte swizzle.
-// Rows are `stride` elements apart.
-bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int heads, int64_t stride, int heads_box, int rows_box) {
+// A map of 16-bit elements with the 128-byte swizzle; strides of all dimensions but the first, in bytes.
+bool make_map(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
   using Encode = decltype(&cuTensorMapEncodeTiled);
   static const Encode encode = [] {
     void* f = nullptr;
@@ -609,10 +615,15 @@ bool make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int heads, 
     return reinterpret_cast<Encode>(f);
   }();
   if (!encode) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(kD), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[2] = {kD * 2, static_cast<cuuint64_t>(stride) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(heads_box), static_cast<cuuint32_t>(rows_box)}, step[3] = {1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  cuuint64_t d[5], s[4];
+  cuuint32_t b[5], step[5];
+  for (int i = 0; i < n; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    step[i] = 1;
+    if (i) s[i - 1] = strides[i - 1];
+  }
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n, const_cast<void*>(base), d, s, b, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

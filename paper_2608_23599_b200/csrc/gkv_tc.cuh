@@ -14,6 +14,8 @@
 #include <stdint.h>
 
 namespace gkv {
+bool make_map(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+
 namespace tc {
 
 constexpr int kSpins = 1 << 20;            // failed polls after which a wait gives up
@@ -66,6 +68,11 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volat
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst), "l"(map),
                "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
                : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {

@@ -14,7 +14,8 @@
 //
 // Work split.  gkv_chunk.h cuts the streams' items (half blocks: 32 tokens) into equal ranges, one per CTA.  The CTA's warps form teams of
 // one warp per 16 rows; a team takes every n-th item of the range and streams it through a ring of its own.  The rings are filled with bulk copies by
-// one warp more, a lane per team.  (The team's first warp needed 1400 cycles of 6100 per half block for that.)
+// one warp more, in which a lane walks the items of each team.  (The team's first warp needed 1400 cycles of 6100 per half block for that.)  Exact
+// rows come 16 at a time by tensor map, two panels of 64 channels with the 128-byte swizzle: copies row by row took 80 cycles each to issue.
 // The teams' results are merged in shared memory in team order, the CTAs' by chunk_merge_kernel.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -34,10 +35,12 @@ constexpr int kVThreads = kVWarps * 32 + 128;
 constexpr int kVLaunchRegs = 128, kVWarpRegs = 152, kVFillRegs = 56;
 static_assert(kVWarps / 4 * kVWarpRegs + kVFillRegs <= (kVWarps / 4 + 1) * kVLaunchRegs, "a split draws on the launch's registers");
 constexpr int kVStage = 5120;              // a 4-bit half block, the keys or the values of an 8-bit one, or of 16 exact rows
-constexpr int kVPitch = kRowBytes + 16;    // exact rows (conflict-free ldmatrix)
+constexpr int kVPitch = kRowBytes + 16;    // centroid rows, copied one by one (conflict-free ldmatrix)
+constexpr int kVPanel = 16 * 128;          // 64 channels of 16 rows that came by tensor map
 constexpr int kVMeta = 96;                 // a stage's description
 constexpr int kVPend = 64;                 // centroids that a team has collected
 constexpr int kVMaxRing = 6;
+constexpr int kVIdle = 1 << 22;            // fruitless looks for room after which the walk gives up
 constexpr int kVOPitch = kD + 4;           // floats of a row in the merge
 constexpr float kVUp = 1048576.f;          // 2^20: what the value accumulators lack (codes are code 2^(p - 24), weights carry 2^(4 - p))
 
@@ -65,11 +68,11 @@ __host__ __device__ inline VLayout verify_layout(int groups) {
   l.meta = l.q + groups * 4096;
   l.pend = l.meta + l.teams * l.ring * kVMeta;
   l.bars = l.pend + l.teams * kVPend * 8;
-  l.bytes = l.bars + l.teams * l.ring * 16 + 16;
+  l.bytes = l.bars + l.teams * l.ring * 16 + 16 + 1024;
   // the merge: every warp's rows, their references and sums
   const int merge = kVWarps * 16 * (kVOPitch + 2) * 4;
   if (l.q < merge) l.q = merge, l.meta = l.q + groups * 4096, l.pend = l.meta + l.teams * l.ring * kVMeta, l.bars = l.pend + l.teams * kVPend * 8,
-                   l.bytes = l.bars + l.teams * l.ring * 16 + 16;
+                   l.bytes = l.bars + l.teams * l.ring * 16 + 16 + 1024;
   return l;
 }
 
@@ -284,70 +287,39 @@ struct VerifyParams {
   int32_t table_stride, walk, n_closed, n_tail, res_items, groups;      // groups: of 16 rows
   float scale_log2;
   ChunkShape s;
+  VLayout lay;
 };
 
-// What one lane does for its team: walks the team's items and fills its ring.
-struct VFill {
-  uint32_t ring, bar_full, bar_free;
-  VMeta* meta;
-  int places, at;
-  uint32_t turn;             // parity of the place's last turn (places that have not been used yet count as freed)
-  volatile uint32_t* abort;
-  // one part; the entry and its bytes
-  __device__ __forceinline__ bool begin(int kind, int level, int n, int causal, uint32_t hide, uint32_t bytes, const float* bias = nullptr) {
-    if (!bar_wait(bar_free + 8 * at, turn, abort)) return false;
-    VMeta& e = meta[at];
-    e.kind = kind;
-    e.level = level;
-    e.n = n;
-    e.causal = causal;
-    e.hide = hide;
-    if (bias)
-      for (int i = 0; i < 16; ++i) e.bias[i] = bias[i < n ? i : 0];
-    if (bytes) bar_expect(bar_full + 8 * at, bytes);
-    return true;
-  }
-  __device__ __forceinline__ void next() {
-    if (++at == places) {
-      at = 0;
-      turn ^= 1u;
-    }
-  }
-  __device__ __forceinline__ bool piece(const uint8_t* src, uint32_t bytes, int kind, int level, uint32_t hide) {
-    if (!begin(kind, level, 0, -1, hide, bytes)) return false;
-    bulk_load(ring + at * kVStage, src, bytes, bar_full + 8 * at);
-    next();
-    return true;
-  }
-  // 16 rows (those that are not there: the first one again, their keys are masked)
-  __device__ __forceinline__ bool rows(const uint8_t* src, uint32_t stride, int n, int causal, uint32_t hide) {
-    if (!begin(2, 16, n, causal, hide, 16 * kRowBytes)) return false;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) bulk_load(ring + at * kVStage + i * kVPitch, src + (i < n ? static_cast<size_t>(i) * stride : 0), kRowBytes, bar_full + 8 * at);
-    next();
-    return true;
-  }
-  __device__ __forceinline__ bool centroids(const uint8_t* arena, const uint32_t* off, const float* bias, int n) {
-    if (!begin(3, 1, n, -1, 0, 16 * kRowBytes, bias)) return false;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) bulk_load(ring + at * kVStage + i * kVPitch, arena + static_cast<size_t>(off[i < n ? i : 0]) * 256, kRowBytes, bar_full + 8 * at);
-    next();
-    return true;
-  }
-  __device__ __forceinline__ bool end() {
-    if (!begin(0, 0, 0, -1, 0, 0)) return false;
-    bar_arrive(bar_full + 8 * at);
-    next();
-    return true;
-  }
+// Rows of 64 channels, two panels each: the arena's (rows of 256 bytes; pairs of such rows, of which one is read), the chunk's keys and values
+struct VerifyMaps {
+  CUtensorMap rows, pairs, k, v;
 };
+
+// A barrier's state, without waiting
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// The next step of a team.  kNone: the walk has to find it; kDone: there is none
+enum : int { kNone = 0, kPiece = 1, kTwoPieces = 2, kSixteenRows = 3, kSixteenCentroids = 4, kNoMore = 5, kDone = 6 };
 
 template <int N>
 __global__ void __launch_bounds__(kVThreads, 1)
-    verify_kernel(const __grid_constant__ VerifyParams p, const __grid_constant__ ChunkCuts cuts, const __grid_constant__ ChunkLens<N> lens) {
-  extern __shared__ __align__(128) uint8_t smem_raw[];
+    verify_kernel(const __grid_constant__ VerifyParams p, const __grid_constant__ ChunkCuts cuts, const __grid_constant__ ChunkLens<N> lens,
+                  const __grid_constant__ VerifyMaps maps) {
+  extern __shared__ uint8_t smem_all[];
+  uint8_t* const smem_raw = smem_all + (1023u & (0u - smem_u32(smem_all)));
   const uint32_t smem = smem_u32(smem_raw);
-  const VLayout lay = verify_layout(p.groups);
+  const VLayout& lay = p.lay;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c4 = lane & 3;
   const bool fills = warp == kVWarps && lane < lay.teams;                 // (the other warps of its four have nothing to do)
   const int team = warp < kVWarps ? warp / p.groups : lane, grp = warp < kVWarps ? warp % p.groups : 0;
@@ -392,73 +364,169 @@ __global__ void __launch_bounds__(kVThreads, 1)
 
   if (warp >= kVWarps) {
     fewer_regs<kVFillRegs>();
-    VFill fill{ring, bar_full, bar_free, meta, lay.ring, 0, 1u, abort};
+    int put_at = 0;                        // the ring's next place, and the parity of its last turn (places not used yet count as freed)
+    uint32_t put_turn = 1;
     for (int from = t0; next_part(from, x); from = x.tile + 1) {
     const int tile = x.tile, b = x.b, h = x.h, len = x.len, begin = x.begin, end = x.end;
     __syncthreads();                       // (barriers are initialised; the previous stream's merge has been read)
-    if (fills) {
-      // ---- the walk of one team ----
+    if (warp == kVWarps) {
+      // ---- the walks, a lane per team ----
       const TableEntry* table = p.table + static_cast<size_t>(tile) * p.table_stride;
       const int blocks_end = 2 * p.n_closed, tail_end = blocks_end + (p.n_tail + 31) / 32, res_end = tail_end + p.res_items;
-      uint32_t* const pend_off = reinterpret_cast<uint32_t*>(smem_raw + lay.pend) + team * kVPend * 2;
+      uint32_t* const pend_off = reinterpret_cast<uint32_t*>(smem_raw + lay.pend) + (fills ? team : 0) * kVPend * 2;
       float* const pend_bias = reinterpret_cast<float*>(pend_off + kVPend);
-      int pend = 0;
-      auto entry = [&](int it) {           // of an item's block
-        return it < min(end, blocks_end) ? *reinterpret_cast<const uint4*>(
-                                               table + static_cast<uint64_t>(it >> 1) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(p.n_closed))
-                                         : make_uint4(0, 0, 0, 0);
+      int pend = 0, it = begin + team;
+      // of an item's block, loaded an item ahead
+      auto entry = [&](int i) {
+        return fills && i < min(end, blocks_end) ? *reinterpret_cast<const uint4*>(
+                                                       table + static_cast<uint64_t>(i >> 1) * static_cast<uint32_t>(p.walk) % static_cast<uint32_t>(p.n_closed))
+                                                 : make_uint4(0, 0, 0, 0);
       };
-      auto row_item = [&](const uint8_t* k, const uint8_t* v, uint32_t stride, int n, int causal, uint32_t hide) {
-        for (int i = 0; ok && i < n; i += 16) {
-          const size_t at = static_cast<size_t>(i) * stride;
-          const int take = min(16, n - i), from = causal < 0 ? -1 : causal + i;
-          ok = fill.rows(k + at, stride, take, from, hide >> i & 0xffffu) && fill.rows(v + at, stride, take, from, 0);
-        }
-      };
-      uint4 e = entry(begin + team);
-      for (int it = begin + team; ok && it < end; it += lay.teams) {
-        if (it < blocks_end) {
-          const uint4 now = e;
-          e = entry(it + lay.teams);
-          const int half = it & 1, level = static_cast<int>(now.y);
-          const uint8_t* at = p.arena + static_cast<size_t>(now.x) * 256;
-          if (level == 1) {
-            if (half) continue;
-            const int n = kBlock - __popc(now.z) - __popc(now.w);
-            pend_off[pend] = now.x;
-            pend_bias[pend] = n > 0 ? lg2(static_cast<float>(n)) / c : -INFINITY;
-            if (++pend == 16) {
-              ok = fill.centroids(p.arena, pend_off, pend_bias, 16) && fill.centroids(p.arena + kRowBytes, pend_off, pend_bias, 16);
-              pend = 0;
+      uint4 e = entry(it);
+      const uint8_t* k = nullptr;                    // the step's codes
+      uint32_t row = 0, hide = 0;                    // first row of what is left of a row item: of the arena, or new token
+      int left = 0, causal = -1, level = 0, source = 0, step = fills ? kNone : kDone;      // source: 0 a block, 1 residual rows, 2 new rows
+      int idle = 0;
+      for (;;) {
+        while (step == kNone) {
+          if (left > 0) {
+            step = kSixteenRows;
+          } else if (pend == 16 || (it >= end && pend > 0)) {
+            step = kSixteenCentroids;
+          } else if (it >= end) {
+            step = kNoMore;
+          } else if (it < blocks_end) {
+            const uint4 now = e;
+            const int half = it & 1;
+            it += lay.teams;
+            e = entry(it);
+            level = static_cast<int>(now.y);
+            hide = half ? now.w : now.z;
+            k = p.arena + static_cast<size_t>(now.x) * 256;
+            if (level == 1) {
+              if (half) continue;
+              const int n = kBlock - __popc(now.z) - __popc(now.w);
+              pend_off[pend] = now.x;
+              pend_bias[pend] = n > 0 ? lg2(static_cast<float>(n)) / c : -INFINITY;
+              ++pend;
+            } else if (level == 16) {
+              row = now.x + half * 32;
+              source = 0;
+              left = 32;
+              causal = -1;
+            } else {
+              k += half * half_bytes(level);
+              step = level == 8 ? kTwoPieces : kPiece;
             }
-          } else if (level == 16) {
-            const uint8_t* k = at + half * 32 * kRowBytes;
-            row_item(k, k + kBlock * kRowBytes, kRowBytes, 32, -1, half ? now.w : now.z);
           } else {
-            const uint32_t bytes = half_bytes(level), hide = half ? now.w : now.z;
-            if (level == 8)
-              ok = fill.piece(at + half * bytes, bytes / 2, 1, 8, hide) && fill.piece(at + half * bytes + bytes / 2, bytes / 2, 1, 8, 0);
-            else ok = fill.piece(at + half * bytes, bytes, 1, level, hide);
+            hide = 0;
+            causal = -1;
+            if (it < tail_end) {
+              const int row0 = (it - blocks_end) * 32;
+              row = table[p.n_closed].off256 + row0;
+              source = 0;
+              left = min(32, p.n_tail - row0);
+            } else if (it < res_end) {
+              const int row0 = (it - tail_end) * 32;
+              row = p.res_off256[tile] + 2 * row0;
+              source = 1;
+              left = max(0, min(32, p.res_count[tile] - row0));
+            } else {
+              const int tok0 = (it - res_end) * 32;
+              row = b * sh.n_new + tok0;
+              source = 2;
+              left = min(32, len - tok0);
+              causal = tok0;
+            }
+            it += lay.teams;
           }
-        } else if (it < tail_end) {
-          const int row0 = (it - blocks_end) * 32;
-          const uint8_t* k = p.arena + static_cast<size_t>(table[p.n_closed].off256) * 256 + row0 * kRowBytes;
-          row_item(k, k + kBlock * kRowBytes, kRowBytes, min(32, p.n_tail - row0), -1, 0);
-        } else if (it < res_end) {
-          const int row0 = (it - tail_end) * 32;
-          const uint8_t* k = p.arena + static_cast<size_t>(p.res_off256[tile]) * 256 + static_cast<size_t>(row0) * 2 * kRowBytes;
-          row_item(k, k + kRowBytes, 2 * kRowBytes, min(32, p.res_count[tile] - row0), -1, 0);
-        } else {
-          const int tok0 = (it - res_end) * 32;
-          const size_t at = ((static_cast<size_t>(b) * sh.n_new + tok0) * sh.n_kv_heads + h) * kRowBytes;
-          row_item(reinterpret_cast<const uint8_t*>(p.k_new) + at, reinterpret_cast<const uint8_t*>(p.v_new) + at, static_cast<uint32_t>(sh.n_kv_heads) * kRowBytes,
-                   min(32, len - tok0), tok0, 0);
+        }
+        __syncwarp();
+        // is there room for the step's one or two parts?
+        const bool two = step == kTwoPieces || step == kSixteenRows || step == kSixteenCentroids;
+        const int at2 = put_at + 1 == lay.ring ? 0 : put_at + 1;
+        const uint32_t turn2 = put_at + 1 == lay.ring ? put_turn ^ 1u : put_turn;
+        const bool ready = step != kDone && bar_test(bar_free + 8 * put_at, put_turn) && (!two || bar_test(bar_free + 8 * at2, turn2));
+        if (__ballot_sync(0xffffffffu, ready) == 0) {
+          if (__all_sync(0xffffffffu, step == kDone)) break;
+          if (++idle > kVIdle) *abort = 1;
+          if (__any_sync(0xffffffffu, *abort != 0)) break;
+          continue;
+        }
+        idle = 0;
+        const uint32_t dst = ring + put_at * kVStage, bar = bar_full + 8 * put_at, dst2 = ring + at2 * kVStage, bar2 = bar_full + 8 * at2;
+        const int n = step == kSixteenCentroids ? pend : min(left, 16);
+        if (ready) {
+          VMeta& m = meta[put_at];
+          m.kind = step == kNoMore ? 0 : step == kSixteenRows ? 2 : step == kSixteenCentroids ? 3 : 1;
+          m.level = level;
+          m.n = n;
+          m.causal = step == kSixteenRows ? causal : -1;
+          m.hide = step == kSixteenCentroids ? 0u : hide;
+          if (step == kNoMore) {
+            bar_arrive(bar);
+          } else if (step == kPiece || step == kTwoPieces) {
+            const uint32_t bytes = step == kPiece ? half_bytes(level) : half_bytes(8) / 2;
+            bar_expect(bar, bytes);
+            bulk_load(dst, k, bytes, bar);
+            if (step == kTwoPieces) {
+              bar_expect(bar2, bytes);
+              bulk_load(dst2, k + bytes, bytes, bar2);
+            }
+          } else if (step == kSixteenRows) {
+            bar_expect(bar, 16 * kRowBytes);
+            bar_expect(bar2, 16 * kRowBytes);
+            if (source == 0) {
+              tma_load_3d(dst, &maps.rows, 0, static_cast<int>(row), 0, bar);
+              tma_load_3d(dst2, &maps.rows, 0, static_cast<int>(row) + kBlock, 0, bar2);
+            } else if (source == 1) {
+              tma_load_4d(dst, &maps.pairs, 0, static_cast<int>(row & 1u), static_cast<int>(row >> 1), 0, bar);
+              tma_load_4d(dst2, &maps.pairs, 0, static_cast<int>((row + 1) & 1u), static_cast<int>((row + 1) >> 1), 0, bar2);
+            } else {
+              tma_load_4d(dst, &maps.k, 0, h, static_cast<int>(row), 0, bar);
+              tma_load_4d(dst2, &maps.v, 0, h, static_cast<int>(row), 0, bar2);
+            }
+          }
+        }
+        // centroids: lane i copies key row i, lane 16 + i value row i (rows that are not there: the first again, their keys are masked)
+        for (uint32_t m = __ballot_sync(0xffffffffu, ready && step == kSixteenCentroids); m; m &= m - 1) {
+          const int t = __ffs(m) - 1, i = lane & 15;
+          const int rows = __shfl_sync(0xffffffffu, n, t);
+          const uint32_t d1 = __shfl_sync(0xffffffffu, dst, t), d2 = __shfl_sync(0xffffffffu, dst2, t);
+          const uint32_t b1 = __shfl_sync(0xffffffffu, bar, t), b2 = __shfl_sync(0xffffffffu, bar2, t);
+          const int place = __shfl_sync(0xffffffffu, put_at, t);
+          const int from = i < rows ? i : 0;
+          const uint32_t* const off = reinterpret_cast<const uint32_t*>(smem_raw + lay.pend) + t * kVPend * 2;
+          const uint8_t* src = p.arena + static_cast<size_t>(off[from]) * 256 + (lane >> 4) * kRowBytes;
+          if (lane < 16) (reinterpret_cast<VMeta*>(smem_raw + lay.meta) + t * lay.ring + place)->bias[i] = reinterpret_cast<const float*>(off + kVPend)[from];
+          __syncwarp();
+          if (lane == t) {
+            bar_expect(b1, 16 * kRowBytes);
+            bar_expect(b2, 16 * kRowBytes);
+          }
+          __syncwarp();
+          bulk_load((lane < 16 ? d1 : d2) + i * kVPitch, src, kRowBytes, lane < 16 ? b1 : b2);
+        }
+        __syncwarp();
+        if (ready) {
+          if (step == kSixteenRows) {
+            left -= n;
+            hide >>= 16;
+            row += source == 1 ? 32 : 16;
+            if (causal >= 0) causal += 16;
+          } else if (step == kSixteenCentroids) {
+            pend = 0;
+          }
+          for (int i = 0; i < (two ? 2 : 1); ++i)
+            if (++put_at == lay.ring) {
+              put_at = 0;
+              put_turn ^= 1u;
+            }
+          step = step == kNoMore ? kDone : kNone;
         }
       }
-      if (ok && pend > 0) ok = fill.centroids(p.arena, pend_off, pend_bias, pend) && fill.centroids(p.arena + kRowBytes, pend_off, pend_bias, pend);
-      ok = ok && fill.end();
-      if (!ok)                             // what is on its way arrives before the memory is used otherwise
-        for (int i = 0; i < lay.ring; ++i) bar_drain(bar_full + 8 * i, i < fill.at ? fill.turn ^ 1u : fill.turn);
+      if (fills && *abort)                   // what is on its way arrives before the memory is used otherwise
+        for (int i = 0; i < lay.ring; ++i) bar_drain(bar_full + 8 * i, i < put_at ? put_turn ^ 1u : put_turn);
     }
     __syncwarp();
     __syncthreads();
@@ -542,22 +610,28 @@ __global__ void __launch_bounds__(kVThreads, 1)
           }
           free_part();
         } else {
-          // 16 rows of bf16: keys [token][channel] are B fragments as they are, values with the transposing load
+          // 16 rows of bf16: keys [token][channel] are B fragments as they are, values with the transposing load.  Chunk i of a row lies in
+          // panel i / 8; where the rows came by tensor map the chunks of a panel are swizzled
+          const bool swizzled = kind == 2;
+          const int panel = swizzled ? kVPanel : 128, pitch = swizzled ? 128 : kVPitch;
           float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-          const uint32_t km = raw + ((lane & 7) + (lane >> 4) * 8) * kVPitch + (lane >> 3 & 1) * 16;
-#pragma unroll 2
-          for (int s = 0; s < 8; ++s) {
-            const uint4 qv = lds128(q + (s * 32 + lane) * 16);
-            uint32_t a[4];
+          {
+            const int row = (lane & 7) + (lane >> 4) * 8;
+            const uint32_t at = raw + row * pitch, flip = swizzled ? (row & 7) << 4 : 0, hi = (lane >> 3 & 1) << 4;
+#pragma unroll 4
+            for (int s = 0; s < 8; ++s) {
+              const uint4 qv = lds128(q + (s * 32 + lane) * 16);
+              uint32_t a[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float2 f = __half22float2(h2(pick(qv, k)));      // (the rows are bf16 by origin: exact)
-              a[k] = bf16_pair(f.x, f.y);
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = __half22float2(h2(pick(qv, k)));      // (the rows are bf16 by origin: exact)
+                a[k] = bf16_pair(f.x, f.y);
+              }
+              uint32_t kb[4];
+              ldmatrix4<false>(kb, at + (s >> 2) * panel + (((s & 3) * 32 + hi) ^ flip));
+              mma_bf16(x[0], a, kb[0], kb[1]);
+              mma_bf16(x[1], a, kb[2], kb[3]);
             }
-            uint32_t kb[4];
-            ldmatrix4<false>(kb, km + s * 32);
-            mma_bf16(x[0], a, kb[0], kb[1]);
-            mma_bf16(x[1], a, kb[2], kb[3]);
           }
           const int n = e.n, causal = e.causal;
           const uint32_t hide = e.hide;
@@ -582,14 +656,24 @@ __global__ void __launch_bounds__(kVThreads, 1)
           const float down = 1.f / kVUp;
           const uint32_t a[4] = {bf16_pair(x[0][0] * down, x[0][1] * down), bf16_pair(x[0][2] * down, x[0][3] * down), bf16_pair(x[1][0] * down, x[1][1] * down),
                                  bf16_pair(x[1][2] * down, x[1][3] * down)};
-          const uint32_t vm = ring + got_at * kVStage + (lane & 15) * kVPitch + (lane >> 4) * 16;
+          const uint32_t vraw = ring + got_at * kVStage;
+          if (swizzled && n < 16) {          // rows that are not there may hold anything: zeros (every warp of the team writes the same ones)
+            for (int i = n * 8 + lane; i < 128; i += 32) {
+              sts128(vraw + i * 16, make_uint4(0, 0, 0, 0));
+              sts128(vraw + kVPanel + i * 16, make_uint4(0, 0, 0, 0));
+            }
+            __syncwarp();
+          }
+          const int vrow = lane & 15;
+          const uint32_t at = vraw + vrow * pitch, flip = swizzled ? (vrow & 7) << 4 : 0, hi = (lane >> 4) << 4;
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
             uint32_t vb[4];
-            ldmatrix4<true>(vb, vm + g * 32);
+            ldmatrix4<true>(vb, at + (g >> 2) * panel + (((g & 3) * 32 + hi) ^ flip));
             mma_bf16(st.o[2 * g], a, vb[0], vb[1]);
             mma_bf16(st.o[2 * g + 1], a, vb[2], vb[3]);
           }
+          if (swizzled && n < 16) fence_async();      // (copies land there next)
           free_part();
         }
       }
@@ -671,7 +755,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
 }
 
 template <int N>
-cudaError_t launch_as(const VerifyParams& p, const ChunkCuts& cuts, const ChunkCall& call, const int32_t* len, cudaStream_t st) {
+cudaError_t launch_as(const VerifyParams& p, const VerifyMaps& maps, const ChunkCuts& cuts, const int32_t* len, cudaStream_t st) {
   ChunkLens<N> lens;
   for (int b = 0; b < (N == 1 ? 1 : p.s.batch); ++b) lens.len[b] = len ? len[b] : p.s.n_new;
   static std::atomic<uint64_t> done{0};
@@ -679,7 +763,7 @@ cudaError_t launch_as(const VerifyParams& p, const ChunkCuts& cuts, const ChunkC
   for (int g = 1; g <= kVerifyRows / 16; ++g) most = std::max(most, static_cast<size_t>(verify_layout(g).bytes));
   const cudaError_t e = raise_smem_limit(verify_kernel<N>, most, done);
   if (e != cudaSuccess) return e;
-  verify_kernel<N><<<cuts.n, kVThreads, verify_layout(p.groups).bytes, st>>>(p, cuts, lens);
+  verify_kernel<N><<<cuts.n, kVThreads, p.lay.bytes, st>>>(p, cuts, lens, maps);
   return cudaGetLastError();
 }
 
@@ -708,7 +792,16 @@ cudaError_t launch_verify(const ChunkCall& call, const ChunkCuts& cuts, const Ch
   p.groups = (call.shape.n_new * call.shape.group + 15) / 16;
   p.scale_log2 = call.scale * kLog2e;
   p.s = call.shape;
-  const cudaError_t e = len && p.s.batch > 1 ? launch_as<kChunkMaxBatch>(p, cuts, call, len, st) : launch_as<1>(p, cuts, call, len, st);
+  p.lay = verify_layout(p.groups);
+  VerifyMaps maps;
+  const uint64_t units = call.arena_bytes / 256, kv = static_cast<uint64_t>(p.s.n_kv_heads), tokens = static_cast<uint64_t>(p.s.batch) * p.s.n_new;
+  const uint64_t rows[3] = {64, units, 2}, rows_step[2] = {256, 128}, pairs[4] = {64, 2, units / 2, 2}, pairs_step[3] = {256, 512, 128};
+  const uint64_t fresh[4] = {64, kv, tokens, 2}, fresh_step[3] = {256, kv * 256, 128};
+  const uint32_t rows_box[3] = {64, 16, 2}, box[4] = {64, 1, 16, 2};
+  if (!make_map(&maps.rows, p.arena, 3, rows, rows_step, rows_box) || !make_map(&maps.pairs, p.arena, 4, pairs, pairs_step, box) ||
+      !make_map(&maps.k, p.k_new, 4, fresh, fresh_step, box) || !make_map(&maps.v, p.v_new, 4, fresh, fresh_step, box))
+    return cudaErrorInvalidValue;
+  const cudaError_t e = len && p.s.batch > 1 ? launch_as<kChunkMaxBatch>(p, maps, cuts, len, st) : launch_as<1>(p, maps, cuts, len, st);
   return e != cudaSuccess ? e : launch_chunk_merge(call, merge, len, st);
 }
 
