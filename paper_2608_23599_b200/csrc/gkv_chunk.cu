@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     *abort = 0;
     bar_init_fence();
   }
+  pdl_launch();
   if (warp == 20) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
   tmem_before();
   __syncthreads();
@@ -820,16 +821,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
 
 // Merges the slots of tiles that were cut (or hold copies of their rows): a warp per row, four channels per lane, slots in order.
 template <int N>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ ChunkMerge merge,
+__global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ ChunkMerge merge,
                                                           const __grid_constant__ ChunkLens<N> lens) {
   const ChunkShape& sh = p.s;
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, rows = kChunkRows / sh.copies;
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31, rows = kChunkRows / sh.copies;
   const int tile = merge.tile[blockIdx.y], first = merge.slot[blockIdx.y], n = (merge.slot[blockIdx.y + 1] - first) * sh.copies;
   const int rt = tile % sh.row_tiles, stream = tile / sh.row_tiles, b = stream / sh.n_kv_heads, h = stream % sh.n_kv_heads;
   const int tok = rt * sh.tile_tokens + row / sh.group;
   if (row >= sh.tile_tokens * sh.group || tok >= lens.len[N == 1 ? 0 : b]) return;
   // part i: copy i % copies of slot first + i / copies
   auto index = [&](int i) { return static_cast<size_t>(first + i / sh.copies) * kChunkRows + (i % sh.copies) * rows + row; };
+  pdl_wait();
   float top = -INFINITY;
   for (int i = lane; i < n; i += 32) {
     const float2 v = p.part_ml[index(i)];
@@ -839,17 +841,24 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
   for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   float sum = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float2 v = p.part_ml[index(i)];
-    const float4 x = reinterpret_cast<const float4*>(p.part_o + index(i) * kD)[lane];
-    if (v.y > 0.f) {
-      const float f = ex2(v.x - top);
-      sum += f * v.y;
-      o.x += f * x.x;
-      o.y += f * x.y;
-      o.z += f * x.z;
-      o.w += f * x.w;
+  for (int i0 = 0; i0 < n; i0 += 8) {      // (eight parts' loads in flight)
+    float2 v[8];
+    float4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const size_t at = index(min(i0 + k, n - 1));
+      v[k] = p.part_ml[at];
+      x[k] = reinterpret_cast<const float4*>(p.part_o + at * kD)[lane];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (i0 + k >= n || !(v[k].y > 0.f)) continue;
+      const float f = ex2(v[k].x - top);
+      sum += f * v[k].y;
+      o.x += f * x[k].x;
+      o.y += f * x[k].y;
+      o.z += f * x[k].z;
+      o.w += f * x[k].w;
     }
   }
   const float inv = 1.f / sum;
@@ -917,10 +926,17 @@ cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const Chu
 cudaError_t launch_chunk_merge(const ChunkCall& call, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
   if (merge.n == 0) return cudaSuccess;
   const ChunkParams p = params_of(call, merge.slot[merge.n]);
-  const dim3 grid((std::min(p.s.tile_tokens * p.s.group, kChunkRows / p.s.copies) + 7) / 8, merge.n);
-  if (one_len(call, len)) chunk_merge_kernel<1><<<grid, 256, 0, st>>>(p, merge, lens_of<1>(call, len));
-  else chunk_merge_kernel<kChunkMaxBatch><<<grid, 256, 0, st>>>(p, merge, lens_of<kChunkMaxBatch>(call, len));
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((std::min(p.s.tile_tokens * p.s.group, kChunkRows / p.s.copies) + 3) / 4, merge.n);
+  cfg.blockDim = dim3(128);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return one_len(call, len) ? cudaLaunchKernelEx(&cfg, chunk_merge_kernel<1>, p, merge, lens_of<1>(call, len))
+                            : cudaLaunchKernelEx(&cfg, chunk_merge_kernel<kChunkMaxBatch>, p, merge, lens_of<kChunkMaxBatch>(call, len));
 }
 
 }  // namespace gkv

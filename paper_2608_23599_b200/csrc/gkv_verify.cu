@@ -16,7 +16,7 @@
 // one warp per 16 rows; a team takes every n-th item of the range and streams it through a ring of its own.  The rings are filled with bulk copies by
 // one warp more, in which a lane walks the items of each team.  (The team's first warp needed 1400 cycles of 6100 per half block for that.)  Exact
 // rows come 16 at a time by tensor map, two panels of 64 channels with the 128-byte swizzle: copies row by row took 80 cycles each to issue.
-// The teams' results are merged in shared memory in team order, the CTAs' by chunk_merge_kernel.
+// The teams' results are merged in shared memory in team order, the CTAs' by chunk_merge_kernel, whose launch overlaps.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -37,19 +37,18 @@ static_assert(kVWarps / 4 * kVWarpRegs + kVFillRegs <= (kVWarps / 4 + 1) * kVLau
 constexpr int kVStage = 5120;              // a 4-bit half block, the keys or the values of an 8-bit one, or of 16 exact rows
 constexpr int kVPitch = kRowBytes + 16;    // centroid rows, copied one by one (conflict-free ldmatrix)
 constexpr int kVPanel = 16 * 128;          // 64 channels of 16 rows that came by tensor map
-constexpr int kVMeta = 96;                 // a stage's description
+constexpr int kVMeta = 80;                 // a stage's description
 constexpr int kVPend = 64;                 // centroids that a team has collected
 constexpr int kVMaxRing = 6;
+constexpr float kVAbove = 4.f;             // log2
 constexpr int kVIdle = 1 << 22;            // fruitless looks for room after which the walk gives up
 constexpr int kVOPitch = kD + 4;           // floats of a row in the merge
 constexpr float kVUp = 1048576.f;          // 2^20: what the value accumulators lack (codes are code 2^(p - 24), weights carry 2^(4 - p))
 
-struct VMeta {
-  int32_t kind;              // 0 = no more, 1 = codes, 2 = rows, 3 = centroids
-  int32_t level, n;          // rows of a row step
-  int32_t causal;            // chunk token of its first key, or -1
-  uint32_t hide;             // keys that are served from elsewhere
-  int32_t pad[3];
+struct alignas(16) VMeta {
+  uint32_t what;             // kind (0 = no more, 1 = codes, 2 = rows, 3 = centroids) | level << 8 | rows << 16
+  int32_t causal;            // chunk token of the first key, or -1
+  uint32_t hide, pad;        // keys that are served from elsewhere
   float bias[16];            // kind 3: what the logits get (in units of q . k)
 };
 static_assert(sizeof(VMeta) == kVMeta, "");
@@ -160,7 +159,9 @@ struct VState {
   float m0, m1, l0, l1;      // references of the two rows (units of q . k), this lane's part of their sums
 };
 
-// The reference moves to the maximum (weights stay at most 1: a weight times a value scale of up to 4094 and 2^4 has to fit fp16); x becomes the weights.
+// x becomes the weights exp2(c (x - m)).  They stay at most 1 (a weight times a value scale of up to 4094 and 2^4 has to fit fp16); where the maximum
+// passes the reference m, m goes kVAbove beyond it, so that it does not move again for the next small step (16 rows' accumulators are rescaled for
+// it: without that in four of five steps of a team).
 template <int NT>
 __device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
   float t0 = fmaxf(x[0][0], x[0][1]), t1 = fmaxf(x[0][2], x[0][3]);
@@ -175,7 +176,7 @@ __device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
     t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, d));
   }
   if (__any_sync(0xffffffffu, t0 > st.m0 || t1 > st.m1)) {
-    const float n0 = fmaxf(st.m0, t0), n1 = fmaxf(st.m1, t1);
+    const float above = kVAbove / c, n0 = t0 > st.m0 ? t0 + above : st.m0, n1 = t1 > st.m1 ? t1 + above : st.m1;
     const float f0 = st.m0 == -INFINITY ? 0.f : ex2((st.m0 - n0) * c), f1 = st.m1 == -INFINITY ? 0.f : ex2((st.m1 - n1) * c);
     st.m0 = n0;
     st.m1 = n1;
@@ -332,6 +333,11 @@ __global__ void __launch_bounds__(kVThreads, 1)
   const uint32_t bar_full = smem + lay.bars + mine * lay.ring * 16, bar_free = bar_full + 8 * lay.ring;
   VMeta* const meta = reinterpret_cast<VMeta*>(smem_raw + lay.meta) + mine * lay.ring;
   if (threadIdx.x == 0) *abort = 0;
+  if (threadIdx.x == kVThreads - 1) {
+    prefetch_map(&maps.rows);
+    prefetch_map(&maps.k);
+    prefetch_map(&maps.v);
+  }
   if (fills) {
     for (int i = 0; i < lay.ring; ++i) {
       bar_init(bar_full + 8 * i, 1);
@@ -361,6 +367,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
     return false;
   };
   Part x;
+  pdl_launch();                            // (the merge waits for the whole grid; its blocks may take their places)
 
   if (warp >= kVWarps) {
     fewer_regs<kVFillRegs>();
@@ -458,11 +465,8 @@ __global__ void __launch_bounds__(kVThreads, 1)
         const int n = step == kSixteenCentroids ? pend : min(left, 16);
         if (ready) {
           VMeta& m = meta[put_at];
-          m.kind = step == kNoMore ? 0 : step == kSixteenRows ? 2 : step == kSixteenCentroids ? 3 : 1;
-          m.level = level;
-          m.n = n;
-          m.causal = step == kSixteenRows ? causal : -1;
-          m.hide = step == kSixteenCentroids ? 0u : hide;
+          const uint32_t kind = step == kNoMore ? 0 : step == kSixteenRows ? 2 : step == kSixteenCentroids ? 3 : 1;
+          *reinterpret_cast<uint4*>(&m) = make_uint4(kind | level << 8 | n << 16, step == kSixteenRows ? causal : -1, step == kSixteenCentroids ? 0u : hide, 0u);
           if (step == kNoMore) {
             bar_arrive(bar);
           } else if (step == kPiece || step == kTwoPieces) {
@@ -579,7 +583,8 @@ __global__ void __launch_bounds__(kVThreads, 1)
       for (;;) {
         if (!(ok = wait_part())) break;
         const VMeta& e = meta[got_at];
-        const int kind = e.kind, level = e.level;
+        const uint4 m = *reinterpret_cast<const uint4*>(&e);
+        const int kind = m.x & 255u, level = m.x >> 8 & 255u;
         const uint32_t raw = ring + got_at * kVStage;
         if (kind == 0) {
           free_part();
@@ -590,7 +595,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
           if (level == 4) code_logits<4>(x, raw, q, lane);
           else if (level == 8) code_logits<8>(x, raw, q, lane);
           else code_logits<2>(x, raw, q, lane);
-          const uint32_t hide = e.hide;
+          const uint32_t hide = m.z;
           if (hide) {
 #pragma unroll
             for (int n = 0; n < 4; ++n)
@@ -633,8 +638,8 @@ __global__ void __launch_bounds__(kVThreads, 1)
               mma_bf16(x[1], a, kb[2], kb[3]);
             }
           }
-          const int n = e.n, causal = e.causal;
-          const uint32_t hide = e.hide;
+          const int n = m.x >> 16, causal = static_cast<int>(m.y);
+          const uint32_t hide = m.z;
           if (kind == 3) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -715,6 +720,12 @@ __global__ void __launch_bounds__(kVThreads, 1)
     fence_async();                         // (copies land there next)
     __syncthreads();
     const int to = chunk_needs_slot(sh, begin, end, items) ? slot++ : -1;
+    auto write_row = [&](int i, const float4& o, float top, float sum) {
+      const size_t at = (static_cast<size_t>(b) * sh.n_new + i / sh.group) * (sh.n_kv_heads * sh.group) + h * sh.group + i % sh.group;
+      const float inv = 1.f / sum;
+      reinterpret_cast<uint2*>(p.out + at * kD)[lane] = make_uint2(bf16_pair(o.x * inv, o.y * inv), bf16_pair(o.z * inv, o.w * inv));
+      if (p.lse && lane == 0) p.lse[at] = (top + lg2(sum)) * kLn2;
+    };
     for (int i = warp; i < rows; i += kVWarps) {           // a warp per row, four channels per lane; lane t has team t's factor
       const int at0 = (i >> 4) * 16 + (i & 15), step = p.groups * 16;
       const float2 v = lane < lay.teams ? mml[at0 + lane * step] : make_float2(0.f, 0.f);
@@ -742,10 +753,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
         reinterpret_cast<float4*>(p.part_o + at * kD)[lane] = o;
         if (lane == 0) p.part_ml[at] = make_float2(top, sum);
       } else {
-        const size_t at = (static_cast<size_t>(b) * sh.n_new + i / sh.group) * (sh.n_kv_heads * sh.group) + h * sh.group + i % sh.group;
-        const float inv = 1.f / sum;
-        reinterpret_cast<uint2*>(p.out + at * kD)[lane] = make_uint2(bf16_pair(o.x * inv, o.y * inv), bf16_pair(o.z * inv, o.w * inv));
-        if (p.lse && lane == 0) p.lse[at] = (top + lg2(sum)) * kLn2;
+        write_row(i, o, top, sum);
       }
     }
     if (!ok) atomicOr(p.status, kStatusInternal);
