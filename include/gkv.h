@@ -184,8 +184,9 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
  *   k_new, v_new  device bf16 [batch][n_new][n_kv_heads][128], 16-byte aligned
  *   len    HOST int32 [batch], 0 .. n_new: real tokens of each sequence (the rest of its rows is neither read for a result nor
  *          written), read during the call only; or NULL = n_new everywhere.  At most 1024 sequences with lengths (GKV_ERR_UNSUPPORTED)
- *   out    device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned: rounded once from fp32 accumulators; weights enter the
- *          value product with 8 (exact rows) or 11 (quantised blocks) bits, quantised keys and values with 11
+ *          (values within +-65504, the cache's exact rows too: rows become fp16 where there are many; larger ones are clamped there)
+ *   out    device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned: rounded once from fp32 accumulators.  Weights enter the value product with
+ *          8 bits or more, values with 11; keys and logits keep 22
  *   lse    device fp32 [batch][n_new][n_q_heads], natural-log sum of exp(logit), or NULL
  *   workspace  device, 16-byte aligned, gkv_chunk_workspace_bytes long: partial results of the call, free again when its kernels
  *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too)
@@ -194,8 +195,11 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
 GKV_API int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len,
                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace that are enough for every gkv_chunk_attn of n_new tokens (below 20 MB).  bytes: host out. */
-GKV_API int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t n_new, size_t* bytes);
+/* Bytes of workspace that a gkv_chunk_attn of n_new tokens over the present context of `layer` works best with.  Few rows (n_new times the
+ * query heads of a KV head up to 64) need less than 20 MB.  More rows have the cache written out as fp16 rows first, 768 bytes per token and KV head: the
+ * answer is what all sequences need, or a number of them at a time that stays below 1 GiB (at least one).  A smaller workspace is
+ * taken as long as it holds one sequence, with as many sequences at a time as it holds (GKV_ERR_INVALID_ARG below that).  bytes: host out. */
+GKV_API int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t* bytes);
 
 /* ---- the prompt: attention and token masses before the ingest ----
  * Packed sequences of one layer: sequence s has the rows [offsets[s], offsets[s + 1]) of every buffer; a sequence may be

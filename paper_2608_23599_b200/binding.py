@@ -109,7 +109,7 @@ def load():
     lib.gkv_debug_export_scores.argtypes = [vp, i32, vp, vp, vp]
     lib.gkv_quest_select_static.argtypes = [vp, i32, vp, i32, vp, C.POINTER(i32), vp]
     lib.gkv_chunk_attn.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
-    lib.gkv_chunk_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+    lib.gkv_chunk_workspace_bytes.argtypes = [vp, i32, i32, C.POINTER(sz)]
     lib.gkv_prompt_attn.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, vp, vp, vp]
     lib.gkv_prompt_mass.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, i32, vp, vp]
     lib.gkv_bits_report.argtypes = [vp, i32, C.POINTER(GkvBits)]
@@ -326,7 +326,7 @@ class Cache:
         h = C.c_void_p()
         _check(load().gkv_create(C.byref(cfg), self._arena_ptr, nbytes, C.byref(h)), "gkv_create")
         self.handle = h
-        self._chunk_bytes, self._chunk_spaces = {}, {}
+        self._chunk_spaces = {}
 
     def close(self):
         self._chunk_spaces = {}
@@ -377,9 +377,9 @@ class Cache:
                                                 _ptr(certificate), self._st())
         return rc if rc == OK else _check(rc, "gkv_decode_attn_observe")
 
-    def gkv_chunk_workspace_bytes(self, n_new) -> int:
+    def gkv_chunk_workspace_bytes(self, layer, n_new) -> int:
         n = C.c_size_t(0)
-        _check(load().gkv_chunk_workspace_bytes(self.handle, n_new, C.byref(n)), "gkv_chunk_workspace_bytes")
+        _check(load().gkv_chunk_workspace_bytes(self.handle, layer, n_new, C.byref(n)), "gkv_chunk_workspace_bytes")
         return n.value
 
     def gkv_chunk_attn(self, layer, q, k_new, v_new, out, lse=None, lengths=None, workspace=None):
@@ -388,7 +388,7 @@ class Cache:
         None; lengths: host ints [B] (rows from there on are left as they are) or None; workspace: a cuda tensor of
         gkv_chunk_workspace_bytes bytes, or None (one is taken from torch's allocator for the call)."""
         cfg = self.cfg
-        ws, keep = (workspace, None) if workspace is not None else self._chunk_workspace(q)
+        ws, keep = (workspace, None) if workspace is not None else self._chunk_workspace(layer, q)
         if isinstance(ws, torch.Tensor):
             ws = (ws.data_ptr(), ws.numel() * ws.element_size()) if ws.device == self.arena.device and ws.is_contiguous() else None
         if ws is not None:
@@ -422,15 +422,13 @@ class Cache:
         rc = _on(dev, call)
         return rc if rc == OK else _check(rc, "gkv_chunk_attn")
 
-    def _chunk_workspace(self, q):
+    def _chunk_workspace(self, layer, q):
         """(address, bytes) of a workspace for a chunk like q, and its owner.  One is kept per stream, whose calls follow one another; a captured
         call gets memory of its graph's own."""
         n = q.shape[1] if isinstance(q, torch.Tensor) and q.dim() == 4 else 0
         if n == 0:
             return (None, 0), None
-        need = self._chunk_bytes.get(n)
-        if need is None:
-            need = self._chunk_bytes[n] = self.gkv_chunk_workspace_bytes(n)
+        need = self.gkv_chunk_workspace_bytes(layer, n)
         dev, handle = self.arena.device, self.stream_handle
         st = torch._C._cuda_getCurrentRawStream(dev.index) if handle is None else handle
         capturing = torch._C._cuda_isCurrentStreamCapturing()

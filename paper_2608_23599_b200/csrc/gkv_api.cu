@@ -1964,19 +1964,45 @@ ChunkShape chunk_of(const gkv_cache* c, int32_t n_new) {
   s.n_kv_heads = c->cfg.n_kv_heads;
   s.group = c->group;
   s.n_new = n_new;
-  chunk_shape(&s);
-  s.item_keys = kChunkKeys;
   return s;
 }
 }  // namespace
 
-int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t n_new, size_t* bytes) {
-  if (!c || !bytes || n_new <= 0) return GKV_ERR_INVALID_ARG;
+namespace {
+// Rows that the stream with most has once its blocks are written out: 64 per block, one per centroid, the partial block, residual rows.
+int dense_rows(const gkv_cache* c, const LayerState& L) {
+  int most = 0;
+  for (int s = 0; s < c->n_streams; ++s) {
+    const int8_t* lv = L.level.data() + static_cast<size_t>(s) * c->max_blocks;
+    int cents = 0;
+    for (int b = 0; b < L.n_closed; ++b) cents += lv[b] == 1;
+    most = std::max(most, (L.n_closed - cents) * kBlock + cents + L.n_tail + L.res_count_h[s]);
+  }
+  return most;
+}
+bool few_rows(const gkv_cache* c, int32_t n_new) { return static_cast<int64_t>(n_new) * c->group <= kVerifyRows; }
+// Sequences that go into a workspace together; 0 where not even one does
+int dense_group(const ChunkShape& s, int n_closed, size_t bytes) {
+  const size_t one = dense_bytes(s, n_closed, 1, nullptr);
+  if (bytes < one) return 0;
+  int n = static_cast<int>(std::min<size_t>(s.batch, bytes / one + 1));
+  while (n > 1 && dense_bytes(s, n_closed, n, nullptr) > bytes) --n;
+  return n;
+}
+}  // namespace
+
+int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t* bytes) {
+  if (!c || !bytes || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0) return GKV_ERR_INVALID_ARG;
   if (is_mla(c->cfg)) return GKV_ERR_UNSUPPORTED;
-  const ChunkShape s = chunk_of(c, n_new);
-  // a cut adds a slot; without copies a CTA has at most two
-  const int64_t tiles = static_cast<int64_t>(c->n_streams) * s.row_tiles;
-  *bytes = static_cast<size_t>(std::min<int64_t>(kChunkParts, tiles + kChunkCtas - 1)) * kChunkSlotFloats * sizeof(float);
+  const LayerState& L = c->layers[layer];
+  ChunkShape s = chunk_of(c, n_new);
+  if (few_rows(c, n_new)) {
+    *bytes = static_cast<size_t>(std::min<int64_t>(kChunkParts, static_cast<int64_t>(c->n_streams) + kChunkCtas - 1)) * kChunkSlotFloats * sizeof(float);      // a cut adds a slot
+    return GKV_OK;
+  }
+  dense_shape(&s, dense_rows(c, L));
+  const size_t one = dense_bytes(s, L.n_closed, 1, nullptr);
+  *bytes = dense_bytes(s, L.n_closed, dense_group(s, L.n_closed, std::max(one, kDenseBytes)), nullptr);
   return GKV_OK;
 }
 
@@ -2000,13 +2026,6 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
   call.n_tail = L.n_tail;
   if (L.has_residual)
     for (int s = 0; s < c->n_streams; ++s) call.res_rows = std::max(call.res_rows, L.res_count_h[s]);
-  const bool few = static_cast<int64_t>(n_new) * c->group <= kVerifyRows;
-  call.shape.cache_items = L.n_closed + (L.n_tail > 0) + (call.res_rows + kChunkKeys - 1) / kChunkKeys;
-  if (few) verify_shape(&call.shape, L.n_closed, L.n_tail, call.res_rows);
-  ChunkCuts cuts;
-  ChunkMerge merge;
-  const int slots = chunk_plan(call.shape, len, few ? 6 : 4, &cuts, &merge);
-  if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
   call.arena = c->arena;
   call.arena_bytes = c->arena_bytes;
   call.table = L.table_d;
@@ -2021,7 +2040,20 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
   call.workspace = static_cast<float*>(workspace);
   call.status = c->status_d;
   call.scale = c->scale;
-  CK(c, (few ? launch_verify : launch_chunk)(call, cuts, merge, len, static_cast<cudaStream_t>(stream)));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (few_rows(c, n_new)) {
+    verify_shape(&call.shape, L.n_closed, L.n_tail, call.res_rows);
+    ChunkCuts cuts;
+    ChunkMerge merge;
+    const int slots = chunk_plan(call.shape, len, 6, &cuts, &merge);
+    if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
+    CK(c, launch_verify(call, cuts, merge, len, st));
+    return GKV_OK;
+  }
+  dense_shape(&call.shape, dense_rows(c, L));
+  const int seqs = workspace ? dense_group(call.shape, L.n_closed, workspace_bytes) : 0;
+  if (seqs == 0) return GKV_ERR_INVALID_ARG;
+  for (int b = 0; b < c->cfg.batch; b += seqs) CK(c, launch_dense(call, b, std::min(seqs, c->cfg.batch - b), len, st));
   return GKV_OK;
 }
 

@@ -1,7 +1,7 @@
 // The work of a chunk call (attention of several new tokens per sequence over the graded cache) and how it is cut into CTAs.
 // Host code without CUDA calls: it runs on a host alone as well.
 //
-// A tile is up to 128 rows of one stream: the query heads of `tile_tokens` consecutive new tokens.  It walks the stream's items: those of
+// A tile is up to 128 or 256 rows of one stream: the query heads of `tile_tokens` consecutive new tokens.  It walks the stream's items: those of
 // the cache, then the chunk's own rows in groups of `item_keys` as far as the tile's last token sees them.  All tiles' items are laid end to end and
 // cut into equal ranges, one per CTA, so a CTA has the end of one tile, whole tiles, and the beginning of another.  A tile that was cut leaves
 // partial results in slots; the slots of a tile follow one another.
@@ -12,10 +12,9 @@
 
 namespace gkv {
 
-constexpr int kChunkRows = 128;            // rows of a tile
-constexpr int kChunkKeys = 64;             // keys of a step
+constexpr int kChunkRows = 128;            // rows of a tile, or of half of one
 constexpr int kChunkCtas = 148;            // one CTA per SM: all of its tensor memory, most of its shared memory
-constexpr int kChunkParts = 2 * kChunkCtas;      // most slots of a call, and most tiles to be merged
+constexpr int kChunkParts = 2 * kChunkCtas;      // most slots of a call (a CTA has at most two), and most tiles to be merged
 constexpr int kChunkSlotFloats = kChunkRows * (128 + 2);
 
 constexpr int kChunkMaxBatch = 1024;       // sequences of a call with lengths of their own
@@ -23,7 +22,7 @@ constexpr int kChunkMaxBatch = 1024;       // sequences of a call with lengths o
 struct ChunkShape {
   int32_t batch, n_kv_heads, group, n_new;
   int32_t cache_items, item_keys;
-  int32_t tile_tokens, row_tiles, copies;    // copies: see chunk_shape
+  int32_t tile_tokens, row_tiles, tile_rows;      // tile_rows: of a slot
 };
 
 inline int chunk_len(const ChunkShape& s, const int32_t* len, int b) { return len ? len[b] : s.n_new; }
@@ -35,20 +34,6 @@ inline int chunk_items(const ChunkShape& s, int len, int rt) {
   if (rt * s.tile_tokens >= len) return 0;
   const int seen = (rt + 1) * s.tile_tokens < len ? (rt + 1) * s.tile_tokens : len;
   return s.cache_items + (seen + s.item_keys - 1) / s.item_keys;
-}
-
-// Tile size.  Where all rows of a stream fill at most half or a quarter of a tile, the tile holds them two or four times, and each copy takes
-// its share of a step's keys: the softmax of few rows is then spread over all warps.  Copies are merged with the slots, which
-// every tile then needs, so this is done up to as many streams as CTAs.
-inline void chunk_shape(ChunkShape* s) {
-  s->tile_tokens = kChunkRows / s->group;
-  s->copies = 1;
-  const int rows = s->n_new * s->group;
-  if (s->batch * s->n_kv_heads <= kChunkCtas && rows <= kChunkRows / 2) {
-    s->copies = rows <= kChunkRows / 4 ? 4 : 2;
-    s->tile_tokens = kChunkRows / s->copies / s->group;
-  }
-  s->row_tiles = (s->n_new + s->tile_tokens - 1) / s->tile_tokens;
 }
 
 struct ChunkCuts {
@@ -65,7 +50,7 @@ struct ChunkMerge {
 #if defined(__CUDACC__)
 __host__ __device__
 #endif
-inline bool chunk_needs_slot(const ChunkShape& s, int begin, int end, int items) { return s.copies > 1 || begin > 0 || end < items; }
+inline bool chunk_needs_slot(int begin, int end, int items) { return begin > 0 || end < items; }
 
 // min_items: what a CTA is worth starting for.  Returns the number of slots, or 0 with cuts->n = 0 where there is nothing to do.
 inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, ChunkCuts* cuts, ChunkMerge* merge) {
@@ -99,7 +84,7 @@ inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, Ch
           }
           const int64_t next = c < n_ctas ? total * c / n_ctas : total;
           const int end = static_cast<int>(std::min<int64_t>(items, next - at));
-          if (chunk_needs_slot(s, begin, end, items)) ++slots;
+          if (chunk_needs_slot(begin, end, items)) ++slots;
           begin = end;
         }
         at += items;
@@ -135,8 +120,8 @@ template <int N>
 struct ChunkLens {                          // N = 1: every sequence has n_new rows
   int32_t len[N];
 };
-cudaError_t launch_chunk(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
 cudaError_t launch_verify(const ChunkCall& call, const ChunkCuts& cuts, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
+cudaError_t launch_dense(const ChunkCall& call, int first, int seqs, const int32_t* len, cudaStream_t st);
 cudaError_t launch_chunk_merge(const ChunkCall& call, const ChunkMerge& merge, const int32_t* len, cudaStream_t st);
 #endif
 
@@ -160,9 +145,24 @@ inline int chunk_walk(int n) {
 constexpr int kVerifyRows = 64;
 inline void verify_shape(ChunkShape* s, int n_closed, int n_tail, int res_rows) {
   s->tile_tokens = s->n_new;
-  s->row_tiles = s->copies = 1;
+  s->tile_rows = kChunkRows;
+  s->row_tiles = 1;
   s->item_keys = 32;
   s->cache_items = 2 * n_closed + (n_tail + 31) / 32 + (res_rows + 31) / 32;
 }
+
+// ---- chunks of many rows (gkv_dense.cu): a tile is 256 rows in two halves, an item 128 rows of keys; centroids have a row each ----
+inline void dense_shape(ChunkShape* s, int rows) {      // rows: of the stream that has most
+  s->tile_tokens = 2 * (kChunkRows / s->group);
+  s->tile_rows = 2 * kChunkRows;
+  s->row_tiles = (s->n_new + s->tile_tokens - 1) / s->tile_tokens;
+  s->item_keys = 128;
+  s->cache_items = (rows + 127) / 128;
+}
+struct DensePlaces {
+  size_t k_hi, k_lo, v, q16, bias, flags, order, blocks, parts;
+};
+size_t dense_bytes(const ChunkShape& s, int n_closed, int seqs, DensePlaces* at);
+constexpr size_t kDenseBytes = size_t(1) << 30;      // what a call's workspace stays below, unless one sequence needs more
 
 }  // namespace gkv

@@ -719,7 +719,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
     }
     fence_async();                         // (copies land there next)
     __syncthreads();
-    const int to = chunk_needs_slot(sh, begin, end, items) ? slot++ : -1;
+    const int to = chunk_needs_slot(begin, end, items) ? slot++ : -1;
     auto write_row = [&](int i, const float4& o, float top, float sum) {
       const size_t at = (static_cast<size_t>(b) * sh.n_new + i / sh.group) * (sh.n_kv_heads * sh.group) + h * sh.group + i % sh.group;
       const float inv = 1.f / sum;

@@ -21,7 +21,7 @@ static int check(const ChunkShape& s, const int32_t* len, int min_items) {
   ChunkMerge merge;
   const int slots = chunk_plan(s, len, min_items, &cuts, &merge);
   const int tiles = s.batch * s.n_kv_heads * s.row_tiles;
-  if (s.tile_tokens * s.group * s.copies > kChunkRows || s.tile_tokens < 1 || s.row_tiles * s.tile_tokens < s.n_new) return 1;
+  if (s.tile_tokens * s.group > s.tile_rows || s.tile_tokens < 1 || s.row_tiles * s.tile_tokens < s.n_new) return 1;
   long total = 0;
   for (int t = 0; t < tiles; ++t) total += chunk_items(s, chunk_len(s, len, t / s.row_tiles / s.n_kv_heads), t % s.row_tiles);
   if (total == 0) return slots || cuts.n || merge.n ? 2 : 0;
@@ -43,7 +43,7 @@ static int check(const ChunkShape& s, const int32_t* len, int min_items) {
       if (t != next_tile || begin != next_item) return 6;
       next_item = end;
       mine += end - begin;
-      if (chunk_needs_slot(s, begin, end, items)) of[t].push_back(slot++);
+      if (chunk_needs_slot(begin, end, items)) of[t].push_back(slot++);
     }
     slot_end = slot;
     seen += mine;
@@ -71,10 +71,8 @@ int main() {
     s.group = 1 + upto(7);
     s.n_new = 1 + upto(i % 3 == 0 ? 700 : 20);
     const int n_closed = upto(i % 5 == 0 ? 600 : 12), n_tail = upto(63), res_rows = upto(3) * 50;
-    chunk_shape(&s);
-    s.item_keys = 64;
-    s.cache_items = n_closed + (n_tail > 0) + (res_rows + 63) / 64;
-    if (s.n_new * s.group <= kVerifyRows && upto(1)) verify_shape(&s, n_closed, n_tail, res_rows);
+    if (s.n_new * s.group <= kVerifyRows && upto(3)) verify_shape(&s, n_closed, n_tail, res_rows);
+    else dense_shape(&s, 64 * upto(n_closed) + n_tail + res_rows);
     if (std::gcd(chunk_walk(n_closed + 1), n_closed + 1) != 1) return 2;
     std::vector<int32_t> len(s.batch);
     for (auto& n : len) n = upto(3) ? upto(s.n_new) : 0;

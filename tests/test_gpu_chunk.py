@@ -1,9 +1,10 @@
 """Attention of a chunk of new tokens over the graded cache, against the oracle's reconstruction of the cache in 64 bits.
 
-Bounds.  A quantised key or value is one rounding to fp16 (2^-11 of itself), a weight one to bf16 (2^-8; fp16 over quantised blocks) and
-the output one to bf16.  With A = max_j scale * sum_c |q_c k_jc| a logit is off by at most (2^-11 + 2^-16) A (the second term: 128
-products added in 32 bits), so an output by 2 (2^-11 + 2^-16) A sum_j w_j |v_j| + (2^-8 + 2^-11) sum_j w_j |v_j| + 2^-8 |o|, and
-the log-sum-exp by (2^-11 + 2^-16) A.  Roundings of this kind have no common sign: the whole output is within 4e-3 of its norm.
+Bounds.  A key is the cache's own (codes times a scaled query pair, or an fp16 pair: 2^-21 of itself and less), a logit a sum of 128
+products: with A = max_j scale * sum_c |q_c k_jc| it is off by at most (2^-16 + 2^-21) A (each addition by 2^-23 of the running sum).  A value
+is rounded to fp16 (2^-11), a weight to bf16 or fp16 (2^-8 at most) and the output to bf16 (2^-8 of itself), so it is off by at most
+2 (2^-16 + 2^-21) A ov + (2^-8 + 2^-11) ov + 2^-8 |o| with ov = sum_j w_j |v_j|.  The log-sum-exp is off by (2^-16 + 2^-21) A and its own
+rounding.  Roundings of this kind have no common sign: the whole output is within 4e-3 of its norm, the log-sum-exp within 4e-6.
 """
 import math
 
@@ -68,7 +69,7 @@ def check(out, lse, oc, q, k, v, lengths=None):
     scale = oc.scale
     got, gl = out.float().cpu().double().numpy(), lse.cpu().double().numpy()
     q, k, v = (x.double().numpy() for x in (q, k, v))
-    num = den = 0.0
+    num = den = lnum = lden = 0.0
     for b in range(batch):
         n = n_new if lengths is None else int(lengths[b])
         assert (got[b, n:] == 7).all() and (gl[b, n:] == 7).all(), "rows behind a sequence's last one were written"
@@ -83,12 +84,14 @@ def check(out, lse, oc, q, k, v, lengths=None):
                 rl = top + np.log(np.exp(x - top[:, None]).sum(1))
                 w = np.exp(x - rl[:, None])
                 o, ov = w @ vv, w @ np.abs(vv)
-                slack = (2.0 ** -11 + 2.0 ** -16) * mag + 2.0 ** -20
+                slack = (2.0 ** -16 + 2.0 ** -21) * mag + 2.0 ** -20
                 tol = (2 * slack[:, None] + 2.0 ** -8 + 2.0 ** -11) * ov + 2.0 ** -8 * np.abs(o)
                 err = np.abs(got[b, :n, a] - o)
                 assert (err <= tol * 1.01).all(), f"sequence {b} head {a}: off by {np.nanmax(err - tol):.3e} more than the bound"
                 assert (np.abs(gl[b, :n, a] - rl) <= slack + 2.0 ** -21 * np.abs(rl)).all(), f"sequence {b} head {a}: log-sum-exp off by {np.abs(gl[b, :n, a] - rl).max():.3e}"
                 num, den = num + (err ** 2).sum(), den + (o ** 2).sum()
+                lnum, lden = lnum + ((gl[b, :n, a] - rl) ** 2).sum(), lden + (rl ** 2).sum()
+    assert lnum <= (4e-6) ** 2 * lden, f"log-sum-exp off by {math.sqrt(lnum / lden):.2e} of its norm"
     assert num <= (4e-3) ** 2 * den, f"off by {math.sqrt(num / den):.2e} of the norm"
 
 
@@ -230,7 +233,7 @@ def test_same_bits_every_time_other_stream_and_given_workspace():
     c, oc, g = caches(8, 2, 64 * 50 + 3, seed=16, plan=plan, **EXT)
     x = chunk(g, 1, 30, 8, 2)
     first = run(c, *x)
-    ws = torch.empty(c.gkv_chunk_workspace_bytes(30), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(c.gkv_chunk_workspace_bytes(0, 30), dtype=torch.uint8, device=DEV)
     again = run(c, *x, workspace=ws)
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
@@ -275,5 +278,5 @@ def test_refusals_on_a_gpu():
         c.gkv_chunk_attn(1, q, k, v, out)
     m = B.Cache(B.make_config(1, 1, 16, 1, 576, 512, 256, v_aliases_k=1))
     n = B.C.c_size_t(0)
-    assert B.load().gkv_chunk_workspace_bytes(m.handle, 4, B.C.byref(n)) == B.ERR_UNSUPPORTED
+    assert B.load().gkv_chunk_workspace_bytes(m.handle, 0, 4, B.C.byref(n)) == B.ERR_UNSUPPORTED
     assert B.load().gkv_chunk_attn(m.handle, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), 1, None, out.data_ptr(), None, None, 0, None) == B.ERR_UNSUPPORTED
