@@ -298,11 +298,11 @@ __global__ void __launch_bounds__(kDThreads, 1)
   uint8_t* const base = smem_raw + (smem - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bars = smem + kDOffBar;
-  const uint32_t bar_q = bars, bar_qfree = bars + 8, bar_s = bars + 16, bar_p = bars + 32, bar_o = bars + 48, bar_drain_mma = bars + 64;
-  const uint32_t bar_full = bars + 72, bar_empty = bar_full + 8 * kDStages;
+  const uint32_t bar_q = bars, bar_qfree = bars + 8, bar_s = bars + 16, bar_p = bars + 32, bar_o = bars + 48, bar_drain_mma = bars + 64, bar_pa = bars + 72;
+  const uint32_t bar_full = bars + 88, bar_empty = bar_full + 8 * kDStages;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kDOffBar + 240);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kDOffBar + 244);
-  static_assert(72 + 16 * kDStages <= 240, "room for the barriers");
+  static_assert(88 + 16 * kDStages <= 240, "room for the barriers");
   const ChunkShape& sh = p.s;
 
   if (threadIdx.x == 0) {
@@ -310,6 +310,7 @@ __global__ void __launch_bounds__(kDThreads, 1)
     bar_init(bar_qfree, 1);
     for (int t = 0; t < 2; ++t) {
       bar_init(bar_s + 8 * t, 1);
+      bar_init(bar_pa + 8 * t, 4);
       bar_init(bar_p + 8 * t, 4);
       bar_init(bar_o + 8 * t, 1);
     }
@@ -444,6 +445,12 @@ __global__ void __launch_bounds__(kDThreads, 1)
             pk[k] = f16_pair(a, b);
           }
           tmem_st16(s_tm + 16 * i, pk);
+          if (i == 2) {                      // three quarters of the weights: their product starts while the rest are made
+            tmem_wait_st();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar_pa + 8 * t);
+          }
         }
         float a, b;
         f2_unpack(f2_add(sum0, sum1), a, b);
@@ -543,9 +550,9 @@ __global__ void __launch_bounds__(kDThreads, 1)
             mma_ss(tmem + t * kDRows, a + off, b + off, id_qk, add || k > 0);
           }
         };
-        auto pv = [&](int t, int i, bool first) {
+        auto pv = [&](int t, int i, bool first, int from, int to) {
           const uint64_t b = smem_desc(smem + kDOffStage + (i % kDStages) * kDTile, kDPanel);
-          for (int k = 0; k < kDRows / 16; ++k) mma_ts(tmem + 256 + t * kDRows, tmem + t * kDRows + 8 * k, b + ((k * 16 * 128) >> 4), id_pv, !first || k > 0);
+          for (int k = from; k < to; ++k) mma_ts(tmem + 256 + t * kDRows, tmem + t * kDRows + 8 * k, b + ((k * 16 * 128) >> 4), id_pv, !first || k > 0);
         };
         for (int from = t0; ok && next_part(from, x); from = x.tile + 1) {
           const int halves = x.two ? 2 : 1;
@@ -574,11 +581,15 @@ __global__ void __launch_bounds__(kDThreads, 1)
             low = more && (flag & kHasLow);
             ok = wait_stage(v) && (!more || wait_stage(k)) && (!low || wait_stage(k + 1));
             for (int t = 0; t < halves && ok; ++t) {
+              ok = bar_wait(bar_pa + 8 * t, weights[t] & 1, abort);
+              if (!ok) break;
+              tmem_after();
+              pv(t, v, j == x.begin, 0, 6);
               ok = bar_wait(bar_p + 8 * t, weights[t] & 1, abort);
               if (!ok) break;
               ++weights[t];
               tmem_after();
-              pv(t, v, j == x.begin);
+              pv(t, v, j == x.begin, 6, 8);
               if (!more) {
                 mma_commit(bar_o + 8 * t);
               } else {

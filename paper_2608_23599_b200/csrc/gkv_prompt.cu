@@ -84,11 +84,11 @@ __global__ void __launch_bounds__(kPThreads, 1)
   uint8_t* const base = smem_raw + (smem - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bars = smem + kPOffBar;
-  const uint32_t bar_q = bars, bar_s = bars + 16, bar_p = bars + 32, bar_o = bars + 48, bar_fix = bars + 64, bar_last = bars + 72, bar_drain_mma = bars + 80;
-  const uint32_t bar_full = bars + 88, bar_empty = bar_full + 8 * kPStages;
+  const uint32_t bar_q = bars, bar_s = bars + 16, bar_p = bars + 32, bar_o = bars + 48, bar_fix = bars + 64, bar_last = bars + 72, bar_drain_mma = bars + 80, bar_pa = bars + 88;
+  const uint32_t bar_full = bars + 104, bar_empty = bar_full + 8 * kPStages;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kPOffBar + 240);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kPOffBar + 244);
-  static_assert(88 + 16 * kPStages <= 240, "room for the barriers");
+  static_assert(104 + 16 * kPStages <= 240, "room for the barriers");
 
   const int head = blockIdx.x % p.n_kv_heads, item = blockIdx.x / p.n_kv_heads;
   const int si = find_seq(seqs, item);
@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
     for (int t = 0; t < 2; ++t) {
       bar_init(bar_q + 8 * t, 1);
       bar_init(bar_s + 8 * t, 1);
+      bar_init(bar_pa + 8 * t, 4);
       bar_init(bar_p + 8 * t, 4);
       bar_init(bar_o + 8 * t, 1);
     }
@@ -205,6 +206,12 @@ __global__ void __launch_bounds__(kPThreads, 1)
           pk[k] = bf16_pair(a, b);
         }
         tmem_st16(s_tm + 16 * i, pk);
+        if (i == 2) {                        // three quarters of the weights: their product starts while the rest are made
+          tmem_wait_st();
+          tmem_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar_pa + 8 * t);
+        }
       }
       float a, b;
       f2_unpack(f2_add(sum0, sum1), a, b);
@@ -275,9 +282,9 @@ __global__ void __launch_bounds__(kPThreads, 1)
           }
           mma_commit(bar_s + 8 * t);
         };
-        auto pv = [&](int t, int i, bool first) {
+        auto pv = [&](int t, int i, bool first, int from, int to) {
           const uint64_t b = smem_desc(smem + kPOffStage + (i % kPStages) * kTileBytes, kPanel);
-          for (int k = 0; k < kRows / 16; ++k) mma_ts(tmem + 256 + t * kRows, tmem + t * kRows + 8 * k, b + ((k * 16 * 128) >> 4), id_pv, !first || k > 0);
+          for (int k = from; k < to; ++k) mma_ts(tmem + 256 + t * kRows, tmem + t * kRows + 8 * k, b + ((k * 16 * 128) >> 4), id_pv, !first || k > 0);
         };
         bool ok = bar_wait(bar_q, 0, abort) && wait_stage(0);
         if (ok) {
@@ -300,10 +307,14 @@ __global__ void __launch_bounds__(kPThreads, 1)
           for (int t = 0; t < 2 && ok; ++t) {
             const int n_t = t ? n1 : n0;
             if (j < n_t) {
+              ok = bar_wait(bar_pa + 8 * t, j & 1, abort);
+              if (!ok) break;
+              tmem_after();
+              pv(t, v, j == 0, 0, 6);
               ok = bar_wait(bar_p + 8 * t, j & 1, abort);
               if (!ok) break;
               tmem_after();
-              pv(t, v, j == 0);
+              pv(t, v, j == 0, 6, 8);
               if (j + 1 == n_t) mma_commit(bar_o + 8 * t);
               else qk(t, k);
             }
