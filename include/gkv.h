@@ -217,12 +217,17 @@ typedef struct gkv_prompt {
 } gkv_prompt;
 
 /* Causal attention of every query head over the exact rows of its own sequence (Sec. 3.1, Eq. 1 before anything is demoted):
- * query row i attends to rows 0 .. i of its sequence.  No workspace; the call is asynchronous and may be captured into a graph.
+ * query row i attends to rows 0 .. i of its sequence.  The call is asynchronous and may be captured into a graph.
  *   q    device bf16 [rows][n_q_heads][128]      k, v  device bf16 [rows][n_kv_heads][128]      (16-byte aligned)
  *   out  device bf16 [rows][n_q_heads][128], 16-byte aligned (rounded once, from fp32 accumulators; weights enter the
  *        value product as bf16)
- *   lse  device fp32 [rows][n_q_heads], packed, natural-log sum of exp(logit), or NULL */
-GKV_API int gkv_prompt_attn(const gkv_prompt* p, const void* q, const void* k, const void* v, void* out, float* lse, void* stream);
+ *   lse  device fp32 [rows][n_q_heads], packed, natural-log sum of exp(logit), or NULL
+ *   workspace  device, 16-byte aligned, or NULL.  With gkv_prompt_workspace_bytes of it (0 for many shapes, below 40 MB for all) work whose
+ *        longest part would hold up the rest is cut into equal ranges; with less the result is the same to rounding, later.  Calls that may
+ *        run at the same time need workspaces of their own (two captured graphs too) */
+GKV_API int gkv_prompt_attn(const gkv_prompt* p, const void* q, const void* k, const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream);
+GKV_API int gkv_prompt_workspace_bytes(const gkv_prompt* p, size_t* bytes);      /* bytes: host out */
 
 /* Attention mass of every prompt token (Sec. 3.1, Eq. 2): the softmax weight that the newest min(n_obs, length) queries of its
  * sequence give it, averaged over them and over the query heads of the KV head; a sequence's masses of one KV head sum to 1.

@@ -30,7 +30,7 @@ EXPORTS = [
     "gkv_debug_replan_levels",
     "gkv_quest_select", "gkv_quest_select_static", "gkv_debug_export_boxes", "gkv_debug_export_scores", "gkv_bits_report",
     "gkv_debug_export_block", "gkv_debug_export_residual", "gkv_debug_export_units",
-    "gkv_prompt_attn", "gkv_prompt_mass", "gkv_chunk_attn", "gkv_chunk_workspace_bytes",
+    "gkv_prompt_attn", "gkv_prompt_workspace_bytes", "gkv_prompt_mass", "gkv_chunk_attn", "gkv_chunk_workspace_bytes",
     "gkv_debug_export_levels", "gkv_debug_plan_levels", "gkv_ctx_len", "gkv_strerror", "gkv_last_cuda_error",
 ]
 
@@ -110,7 +110,8 @@ def load():
     lib.gkv_quest_select_static.argtypes = [vp, i32, vp, i32, vp, C.POINTER(i32), vp]
     lib.gkv_chunk_attn.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.gkv_chunk_workspace_bytes.argtypes = [vp, i32, i32, C.POINTER(sz)]
-    lib.gkv_prompt_attn.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, vp, vp, vp]
+    lib.gkv_prompt_attn.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.gkv_prompt_workspace_bytes.argtypes = [C.POINTER(GkvPrompt), C.POINTER(sz)]
     lib.gkv_prompt_mass.argtypes = [C.POINTER(GkvPrompt), vp, vp, vp, i32, vp, vp]
     lib.gkv_bits_report.argtypes = [vp, i32, C.POINTER(GkvBits)]
     lib.gkv_debug_export_block.argtypes = [vp, i32, i32, i32, i32, i32, C.POINTER(i32), vp, vp, vp, vp, C.POINTER(i32)]
@@ -129,8 +130,9 @@ def load():
     from . import _gkv_call
     _gkv_call.bind(*(C.cast(f, vp).value for f in (lib.gkv_append_demote, lib.gkv_decode_attn, lib.gkv_decode_attn_observe,
                                                    lib.gkv_quest_select)), vp)
-    _gkv_call.bind_rows(*(C.cast(f, vp).value for f in (lib.gkv_prompt_attn, lib.gkv_prompt_mass, lib.gkv_chunk_attn)), torch.Tensor, torch.bfloat16,
-                        torch.float32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    _gkv_call.bind_rows(*(C.cast(f, vp).value for f in (lib.gkv_prompt_attn, lib.gkv_prompt_workspace_bytes, lib.gkv_prompt_mass, lib.gkv_chunk_attn)),
+                        torch.Tensor, torch.bfloat16, torch.float32, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+                        torch._C._cuda_isCurrentStreamCapturing)
     _lib, _call = lib, _gkv_call
     return lib
 
@@ -270,11 +272,30 @@ def _on(device, call):
         return call(_stream())
 
 
+_prompt_spaces = {}      # workspaces of prompt attention, one per stream (whose calls follow one another)
+
+
+def _prompt_space(device, need):
+    """(address, bytes, owner): the stream's workspace, or, while it is captured, memory of the graph's own."""
+    with torch.cuda.device(device):
+        key = 64 * _stream() + device.index
+        captured = torch._C._cuda_isCurrentStreamCapturing()
+        kept = None if captured else _prompt_spaces.get(key)
+        if kept is None or kept[1] < need:
+            t = torch.empty(need, dtype=torch.uint8, device=device)
+            kept = t.data_ptr(), need, t
+            if not captured:
+                _prompt_spaces[key] = kept
+    return kept
+
+
 def gkv_prompt_attn(q, k, v, out, offsets, lse=None, softmax_scale=0.0):
     """Causal attention of packed prompts: q, out cuda bf16 [rows][n_q_heads][128], k, v cuda bf16 [rows][n_kv_heads][128]
     (rows may be slices of a fused projection), offsets: host row numbers, sequence s = rows [offsets[s], offsets[s + 1]);
     lse: cuda fp32 [rows][n_q_heads] or None.  Rows of no sequence are left as they are."""
-    rc = (_call or _loaded()).prompt_attn(q, k, v, out, offsets, lse, softmax_scale)
+    rc = (_call or _loaded()).prompt_attn(q, k, v, out, offsets, lse, softmax_scale, _prompt_spaces)
+    if rc is not NotImplemented and rc > 0:      # bytes of workspace
+        rc = _call.prompt_attn(q, k, v, out, offsets, lse, softmax_scale, _prompt_space(q.device, rc))
     if rc == OK:
         return rc
     if rc is not NotImplemented:
@@ -287,7 +308,13 @@ def gkv_prompt_attn(q, k, v, out, offsets, lse=None, softmax_scale=0.0):
         _floats(lse, "lse", 0, q.shape[:2])
     d, _keep = _prompt(q, k, offsets, softmax_scale, v, out, lse)
     d.q_stride, d.k_stride, d.v_stride, d.out_stride = qs, ks, vs, os_
-    rc = _on(q.device, lambda st: load().gkv_prompt_attn(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), st))
+    need = C.c_size_t(0)
+    _check(load().gkv_prompt_workspace_bytes(C.byref(d), C.byref(need)), "gkv_prompt_workspace_bytes")
+
+    def call(st):
+        ws = _prompt_space(q.device, need.value) if need.value else (None, 0)
+        return load().gkv_prompt_attn(C.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), ws[0], ws[1], st)
+    rc = _on(q.device, call)
     return rc if rc == OK else _check(rc, "gkv_prompt_attn")
 
 

@@ -13,7 +13,7 @@ CALL_SOURCE = os.path.join(CSRC, "gkv_call.cpp")         # the binding's extensi
 CALL_LIB = os.path.join(HERE, "_gkv_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["gkv_api.cu", "gkv_decode.cu", "gkv_units.cu", "gkv_pack.cu", "gkv_ingest.cu", "gkv_quest.cu", "gkv_rdplan.cu", "gkv_mla.cu", "gkv_mla_decode.cu", "gkv_prompt.cu", "gkv_chunk.cu", "gkv_verify.cu", "gkv_dense.cu"]
 ABI = os.path.join(CSRC, "..", "..", "include", "gkv.h")
-HEADERS = ["gkv_internal.h", "gkv_exchange.h", "gkv_layout.cuh", "gkv_tc.cuh", "gkv_chunk.h", "gkv_mla.h", ABI]
+HEADERS = ["gkv_internal.h", "gkv_exchange.h", "gkv_layout.cuh", "gkv_tc.cuh", "gkv_chunk.h", "gkv_attend.cuh", "gkv_mla.h", ABI]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",

@@ -18,6 +18,7 @@
 #include "gkv_chunk.h"
 #include "gkv_internal.h"
 #include "gkv_mla.h"
+#include "gkv_tc.cuh"
 
 using namespace gkv;
 
@@ -1957,6 +1958,46 @@ int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, float* o
   return decode_impl(c, layer, q, nullptr, 0, out, lse, true, block_mass, certificate, stream);
 }
 
+// What gkv_tc.cuh and gkv_internal.h declare for the tensor-map kernels
+namespace {
+bool all_on_current_device(std::initializer_list<const void*> ptrs) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  for (const void* p : ptrs) {
+    if (!p) continue;
+    cudaPointerAttributes a{};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+      cudaGetLastError();
+      return false;
+    }
+    if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != dev)) return false;
+  }
+  return true;
+}
+
+bool encode_map(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+  using Encode = decltype(&cuTensorMapEncodeTiled);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found{};
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return false;
+  cuuint64_t d[5], s[4];
+  cuuint32_t b[5], step[5];
+  for (int i = 0; i < n; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    step[i] = 1;
+    if (i) s[i - 1] = strides[i - 1];
+  }
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n, const_cast<void*>(base), d, s, b, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+const bool installed = (on_current_device = all_on_current_device, make_map = encode_map, true);
+}  // namespace
+
 namespace {
 ChunkShape chunk_of(const gkv_cache* c, int32_t n_new) {
   ChunkShape s{};
@@ -2045,7 +2086,7 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
     verify_shape(&call.shape, L.n_closed, L.n_tail, call.res_rows);
     ChunkCuts cuts;
     ChunkMerge merge;
-    const int slots = chunk_plan(call.shape, len, 6, &cuts, &merge);
+    const int slots = chunk_plan(call.shape, len, 6, 0, 0, &cuts, &merge);
     if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
     CK(c, launch_verify(call, cuts, merge, len, st));
     return GKV_OK;

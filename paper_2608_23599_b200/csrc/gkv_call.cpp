@@ -151,6 +151,7 @@ PyObject* py_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // Everything that the binding asks of the arguments is asked here too, without its messages: what is not in order makes the function return
 // NotImplemented, and the binding finds and names the fault.
 decltype(&gkv_prompt_attn) f_prompt_attn = nullptr;
+decltype(&gkv_prompt_workspace_bytes) f_prompt_bytes = nullptr;
 decltype(&gkv_prompt_mass) f_prompt_mass = nullptr;
 decltype(&gkv_chunk_attn) f_chunk = nullptr;
 PyObject* tensor_type = nullptr;     // torch.Tensor
@@ -158,21 +159,23 @@ PyObject* bf16_type = nullptr;       // torch.bfloat16
 PyObject* f32_type = nullptr;        // torch.float32
 PyObject* get_device = nullptr;      // the current device
 PyObject* get_stream = nullptr;      // a device's current stream
+PyObject* capturing = nullptr;       // is it being captured?
 PyObject *s_shape = nullptr, *s_stride = nullptr, *s_dtype = nullptr, *s_get_device = nullptr;
 
-// bind_rows(prompt_attn, prompt_mass, chunk_attn, Tensor, bfloat16, float32, current device, current stream)
+// bind_rows(prompt_attn, prompt_workspace_bytes, prompt_mass, chunk_attn, Tensor, bfloat16, float32, current device, current stream, is it captured)
 PyObject* py_bind_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[3];
-  if (!want(n, 8)) return nullptr;
-  for (int i = 0; i < 3; ++i)
+  void* p[4];
+  if (!want(n, 10)) return nullptr;
+  for (int i = 0; i < 4; ++i)
     if (!as_plain(a[i], &p[i])) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_TypeError, "an address is needed");
   f_prompt_attn = reinterpret_cast<decltype(f_prompt_attn)>(p[0]);
-  f_prompt_mass = reinterpret_cast<decltype(f_prompt_mass)>(p[1]);
-  f_chunk = reinterpret_cast<decltype(f_chunk)>(p[2]);
-  PyObject** const kept[5] = {&tensor_type, &bf16_type, &f32_type, &get_device, &get_stream};
-  for (int i = 0; i < 5; ++i) {
-    Py_INCREF(a[3 + i]);
-    Py_XSETREF(*kept[i], a[3 + i]);
+  f_prompt_bytes = reinterpret_cast<decltype(f_prompt_bytes)>(p[1]);
+  f_prompt_mass = reinterpret_cast<decltype(f_prompt_mass)>(p[2]);
+  f_chunk = reinterpret_cast<decltype(f_chunk)>(p[3]);
+  PyObject** const kept[6] = {&tensor_type, &bf16_type, &f32_type, &get_device, &get_stream, &capturing};
+  for (int i = 0; i < 6; ++i) {
+    Py_INCREF(a[4 + i]);
+    Py_XSETREF(*kept[i], a[4 + i]);
   }
   Py_RETURN_NONE;
 }
@@ -261,9 +264,10 @@ bool describe(gkv_prompt* d, const Rows& q, const Rows& k, const Ints& off, PyOb
   return !PyErr_Occurred();
 }
 
-// prompt_attn(q, k, v, out, offsets, lse, softmax_scale)
+// prompt_attn(q, k, v, out, offsets, lse, softmax_scale, workspaces) -> status, or the bytes of workspace that the caller has to bring.
+// workspaces: a tuple (address, bytes, ...), or a dict of them by 64 * stream + device, which is not looked at while the stream is captured
 PyObject* py_prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!want(n, 7)) return nullptr;
+  if (!want(n, 8)) return nullptr;
   long dev;
   void* st;
   Rows q, k, v, out, lse{};
@@ -275,10 +279,30 @@ PyObject* py_prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !heads_together(out, &d.out_stride) || !shaped(v, k.shape[0], k.shape[1], 128) || !shaped(out, q.shape[0], q.shape[1], 128) ||
       (a[5] != Py_None && (!packed(lse) || !shaped(lse, q.shape[0], q.shape[1], 0))))
     return refuse();
-  int rc;
-  Py_BEGIN_ALLOW_THREADS
-  rc = f_prompt_attn(&d, q.ptr, k.ptr, v.ptr, out.ptr, static_cast<float*>(lse.ptr), st);
-  Py_END_ALLOW_THREADS
+  size_t need = 0, have = 0;
+  void* ws = nullptr;
+  int rc = f_prompt_bytes(&d, &need);
+  if (rc == GKV_OK && need > 0) {
+    PyObject* space = a[7];
+    if (PyDict_Check(space)) {
+      PyObject* busy = PyObject_CallNoArgs(capturing);
+      if (!busy) return nullptr;
+      const bool captured = PyObject_IsTrue(busy) != 0;
+      Py_DECREF(busy);
+      PyObject* key = PyLong_FromUnsignedLongLong((reinterpret_cast<unsigned long long>(st) << 6) + static_cast<unsigned long long>(dev));
+      if (!key) return nullptr;
+      space = captured ? nullptr : PyDict_GetItemWithError(a[7], key);
+      Py_DECREF(key);
+    }
+    if (space && PyTuple_Check(space) && PyTuple_GET_SIZE(space) >= 2 && as_plain(PyTuple_GET_ITEM(space, 0), &ws)) have = PyLong_AsSize_t(PyTuple_GET_ITEM(space, 1));
+    if (PyErr_Occurred()) return refuse();
+    if (have < need) return PyLong_FromSize_t(need);
+  }
+  if (rc == GKV_OK) {
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_prompt_attn(&d, q.ptr, k.ptr, v.ptr, out.ptr, static_cast<float*>(lse.ptr), ws, have, st);
+    Py_END_ALLOW_THREADS
+  }
   return PyLong_FromLong(rc);
 }
 

@@ -1,6 +1,7 @@
 // Merges the parts of tiles that several CTAs of a chunk call worked on (gkv_chunk.h), in the order of their slots.
 #include <cuda_runtime.h>
 
+#include "gkv_attend.cuh"
 #include "gkv_chunk.h"
 #include "gkv_internal.h"
 #include "gkv_tc.cuh"
@@ -29,8 +30,8 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
   const int rt = tile % sh.row_tiles, stream = tile / sh.row_tiles, b = stream / sh.n_kv_heads, h = stream % sh.n_kv_heads;
   const int tok = rt * sh.tile_tokens + row / sh.group;
   if (row >= sh.tile_tokens * sh.group || tok >= lens.len[N == 1 ? 0 : b]) return;
-  auto index = [&](int i) { return static_cast<size_t>(first + i) * sh.tile_rows + row; };
   pdl_wait();
+  auto index = [&](int i) { return static_cast<size_t>(first + i) * sh.tile_rows + row; };
   float top = -INFINITY;
   for (int i = lane; i < n; i += 32) {
     const float2 v = p.part_ml[index(i)];
@@ -70,16 +71,7 @@ template <int N>
 cudaError_t launch_as(const MergeParams& p, const ChunkMerge& merge, const int32_t* len, cudaStream_t st) {
   ChunkLens<N> lens;
   for (int b = 0; b < (N == 1 ? 1 : p.s.batch); ++b) lens.len[b] = len ? len[b] : p.s.n_new;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((p.s.tile_tokens * p.s.group + 3) / 4, merge.n);
-  cfg.blockDim = dim3(128);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<N>, p, merge, lens);
+  return attend::launch_behind(chunk_merge_kernel<N>, dim3((p.s.tile_tokens * p.s.group + 3) / 4, merge.n), 128, 0, st, p, merge, lens);
 }
 
 }  // namespace

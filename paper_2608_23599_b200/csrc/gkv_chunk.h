@@ -52,52 +52,66 @@ __host__ __device__
 #endif
 inline bool chunk_needs_slot(int begin, int end, int items) { return begin > 0 || end < items; }
 
-// min_items: what a CTA is worth starting for.  Returns the number of slots, or 0 with cuts->n = 0 where there is nothing to do.
-inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, ChunkCuts* cuts, ChunkMerge* merge) {
-  int64_t total = 0;
-  for (int b = 0; b < s.batch; ++b) {
-    const int n = chunk_len(s, len, b);
-    for (int rt = 0; rt < s.row_tiles && rt * s.tile_tokens < n; ++rt) total += static_cast<int64_t>(s.n_kv_heads) * chunk_items(s, n, rt);
-  }
+// Cuts `tiles` tiles, tile t of items(t) steps (asked for in order), into ranges of equal cost, one per CTA: a tile costs its steps and `start` more for its
+// beginning, `total` in all.  A cut that would come within `snap` of a tile's beginning or end comes there: a tile that is not cut needs no slots.
+// min_items: what a CTA is worth starting for.  Returns the number of slots; 0 with cuts->n = 0 where there is nothing to do.
+template <class Items>
+inline int cut_tiles(int tiles, int64_t total, int min_items, int start, int snap, Items items, ChunkCuts* cuts, ChunkMerge* merge) {
   cuts->n = 0;
   merge->n = 0;
   merge->slot[0] = 0;
   if (total == 0) return 0;
   const int n_ctas = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / min_items)));
-  // tiles in the order (sequence, KV head, row tile)
+  // where CTAs begin: at the first tile that has steps, then at every n_ctas-th of the cost, places that fall together counted once
   int64_t at = 0;
-  int c = 0, slots = 0, tile = 0;
+  int c = 1, last_tile = -1, last_item = 0;
+  bool to_next = false;                      // a cut was moved to the next tile's beginning
+  auto begin = [&](int tile, int item) {
+    if (last_tile > tile || (last_tile == tile && last_item >= item)) return;
+    cuts->tile[cuts->n] = last_tile = tile;
+    cuts->item[cuts->n++] = last_item = item;
+  };
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int n = items(tile);
+    if (n == 0) continue;
+    if (last_tile < 0 || to_next) begin(tile, 0);
+    to_next = false;
+    for (; c < n_ctas && total * c / n_ctas < at + start + n; ++c) {
+      const int64_t cut = total * c / n_ctas - at - start;
+      if (cut <= snap) begin(tile, 0);
+      else if (cut < n - snap) begin(tile, static_cast<int>(cut));
+      else to_next = true;
+    }
+    at += n + start;
+  }
+  cuts->tile[cuts->n] = tiles;
+  cuts->item[cuts->n] = 0;
+  // their slots
+  int slots = 0;
+  for (int i = 0; i < cuts->n; ++i) {
+    cuts->slot[i] = slots;
+    for (int tile = cuts->tile[i]; tile <= cuts->tile[i + 1] && tile < tiles; ++tile) {
+      const int n = items(tile), from = tile == cuts->tile[i] ? cuts->item[i] : 0, to = tile == cuts->tile[i + 1] ? cuts->item[i + 1] : n;
+      if (from >= to || !chunk_needs_slot(from, to, n)) continue;
+      if (merge->n == 0 || merge->tile[merge->n - 1] != tile) merge->tile[merge->n++] = tile;
+      merge->slot[merge->n] = ++slots;
+    }
+  }
+  return slots;
+}
+
+// Tiles in the order (sequence, KV head, row tile)
+inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap, ChunkCuts* cuts, ChunkMerge* merge) {
+  int64_t total = 0;
   for (int b = 0; b < s.batch; ++b) {
     const int n = chunk_len(s, len, b);
-    for (int h = 0; h < s.n_kv_heads; ++h)
-      for (int rt = 0; rt < s.row_tiles; ++rt, ++tile) {
-        const int items = chunk_items(s, n, rt);
-        if (items == 0) continue;
-        int begin = 0;
-        const int first = slots;
-        while (begin < items) {
-          while (c < n_ctas && at + begin >= total * c / n_ctas) {      // CTA c begins here
-            cuts->tile[c] = tile;
-            cuts->item[c] = begin;
-            cuts->slot[c] = slots;
-            ++c;
-          }
-          const int64_t next = c < n_ctas ? total * c / n_ctas : total;
-          const int end = static_cast<int>(std::min<int64_t>(items, next - at));
-          if (chunk_needs_slot(begin, end, items)) ++slots;
-          begin = end;
-        }
-        at += items;
-        if (slots > first) {
-          merge->tile[merge->n++] = tile;
-          merge->slot[merge->n] = slots;
-        }
-      }
+    for (int rt = 0; rt < s.row_tiles && rt * s.tile_tokens < n; ++rt) {
+      const int items = chunk_items(s, n, rt);
+      if (items) total += static_cast<int64_t>(s.n_kv_heads) * (items + start);
+    }
   }
-  cuts->n = n_ctas;
-  cuts->tile[n_ctas] = s.batch * s.n_kv_heads * s.row_tiles;
-  cuts->item[n_ctas] = 0;
-  return slots;
+  return cut_tiles(s.batch * s.n_kv_heads * s.row_tiles, total, min_items, start, snap,
+                   [&](int tile) { return chunk_items(s, chunk_len(s, len, tile / s.row_tiles / s.n_kv_heads), tile % s.row_tiles); }, cuts, merge);
 }
 
 #if defined(__CUDACC__)

@@ -204,7 +204,9 @@ cudaError_t raise_smem_limit(void (*kernel)(Args...), size_t bytes, std::atomic<
   return e;
 }
 
-bool on_current_device(std::initializer_list<const void*> ptrs);      // null pointers aside
+// Whether all are memory of the current device, or memory that every device reaches (null pointers aside): the tensor-map kernels must not be given
+// another GPU's.  gkv_api.cu sets it when the library is loaded.
+inline bool (*on_current_device)(std::initializer_list<const void*> ptrs) = nullptr;
 
 constexpr uint32_t kStatusRange = 1u;      // a scale or zero saturated
 constexpr uint32_t kStatusInternal = 2u;   // an index check failed inside a kernel

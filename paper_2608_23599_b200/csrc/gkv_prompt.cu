@@ -1,16 +1,7 @@
 // Attention of whole prompts over their own exact rows, and the attention mass that their tokens get from the newest queries
 // (Sec. 3.1, Eq. 2): what a serving program runs before it hands a prompt's rows to the bulk ingest.
 //
-// prompt_kernel.  Causal softmax attention of packed sequences, grouped heads.  A CTA has two row tiles of up to 128 rows; the
-// rows of a tile are the g query heads of 128 / g consecutive tokens, so that all of them read one KV head and the diagonal is
-// 128 / g tokens wide.  Per step of 128 keys and row tile:
-//   S = Q K^T            tcgen05, both operands in shared memory, fp32 accumulator in tensor memory
-//   m' = max(m, row max) the reference m moves only when the maximum has grown by more than 2^8: P then stays below 2^8, and the
-//                        accumulator is rescaled a handful of times per row, not once per step
-//   P = exp2(c S - c m)  bf16 (a rounding of at most 2^-9 of each weight; its sum l is taken before it), over S in tensor memory
-//   O += P V             tcgen05, P from tensor memory, V as it lies ([token][channel], MN-major)
-// While four warps work on one tile's S, the tensor cores work for the other tile: the four products of a step are issued by one
-// thread in the order P0 V, Q0 K, P1 V, Q1 K.  K and V tiles come by TMA through a ring of 32 KB stages.
+// Attention: attend_kernel (gkv_attend.cuh) over tiles of the packed sequences, bf16 operands as they lie.
 //
 // mass_kernel.  S^T = K Q^T for the observing rows: a thread owns a token, so the sum over rows of exp2(c S - lse) needs no
 // exchange, and every sum has a fixed order.  K is read once.
@@ -22,10 +13,13 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
 #include <numeric>
 #include <vector>
 
 #include "../../include/gkv.h"
+#include "gkv_attend.cuh"
+#include "gkv_chunk.h"
 #include "gkv_internal.h"
 #include "gkv_tc.cuh"
 
@@ -34,9 +28,9 @@ namespace {
 
 using namespace tc;
 
-constexpr int kRows = 128;                 // rows of a tile, keys of a step
-constexpr int kPanel = kRows * 128;        // bytes of 64 channels of 128 rows
-constexpr int kTileBytes = 2 * kPanel;
+using attend::kPanel;
+using attend::kRows;
+using attend::kTileBytes;
 constexpr int kMaxSeqs = 1024;             // sequences of one launch
 constexpr int kFewSeqs = 32;               // the same where the parameters are to stay short
 
@@ -58,293 +52,84 @@ __device__ __forceinline__ int find_seq(const Seqs<N>& s, int item) {
 }
 
 // ---- prompt attention ----------------------------------------------------------------------------
-constexpr int kPThreads = 384;             // softmax of tile 0, of tile 1 (four warps each), loads, products, value rows' end, -
-constexpr int kPStages = 5;
-constexpr int kPOffStage = 2 * kTileBytes;
-constexpr int kPOffBar = kPOffStage + kPStages * kTileBytes;
-constexpr int kPSmem = kPOffBar + 256 + 1024;
-constexpr int kPLaunchRegs = 168, kPSoftRegs = 216, kPOtherRegs = 72;
-static_assert(2 * kPSoftRegs + kPOtherRegs <= 3 * kPLaunchRegs, "a split draws on the launch's registers");
-constexpr float kSlack = 8.f;              // log2 of what a weight may exceed 1 by before the reference moves
-
-struct PromptParams {
-  uint16_t* out;
-  float* lse;
-  int64_t out_stride;
-  int32_t n_q_heads, n_kv_heads, group, tile_tokens;
-  float scale_log2;
+// Tiles of a launch in the order (sequence, row tile from the last one on, KV head): those with most keys first.
+template <int N>
+struct Tiles {
+  Seqs<N> seqs;                              // work items: row tiles
+  int32_t n_kv_heads, span;                  // tokens of a tile
+  __host__ __device__ int count() const { return seqs.first[seqs.n] * n_kv_heads; }
+  struct Place {
+    int seq, head, tok0, len;
+  };
+  __device__ __forceinline__ Place place(int tile) const {
+    Place p;
+    p.head = tile % n_kv_heads;
+    const int item = tile / n_kv_heads;
+    p.seq = find_seq(seqs, item);
+    p.len = seqs.len[p.seq];
+    p.tok0 = (seqs.first[p.seq + 1] - 1 - item) * span;
+    return p;
+  }
 };
+__host__ __device__ inline int steps_of(int tok0, int span, int len) { return ((tok0 + span < len ? tok0 + span : len) + kRows - 1) / kRows; }
 
 template <int N>
-__global__ void __launch_bounds__(kPThreads, 1)
-    prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ Seqs<N> seqs, const __grid_constant__ CUtensorMap map_q,
-                  const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* const base = smem_raw + (smem - smem_u32(smem_raw));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t bars = smem + kPOffBar;
-  const uint32_t bar_q = bars, bar_s = bars + 16, bar_p = bars + 32, bar_o = bars + 48, bar_fix = bars + 64, bar_last = bars + 72, bar_drain_mma = bars + 80, bar_pa = bars + 88;
-  const uint32_t bar_full = bars + 104, bar_empty = bar_full + 8 * kPStages;
-  volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kPOffBar + 240);
-  volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kPOffBar + 244);
-  static_assert(104 + 16 * kPStages <= 240, "room for the barriers");
-
-  const int head = blockIdx.x % p.n_kv_heads, item = blockIdx.x / p.n_kv_heads;
-  const int si = find_seq(seqs, item);
-  const int len = seqs.len[si], row0 = seqs.row[si];
-  const int span = 2 * p.tile_tokens;
-  // the last tiles of a sequence, the ones with most keys, first
-  const int tok0 = ((len + span - 1) / span - 1 - (item - seqs.first[si])) * span;
-  // keys that tile t needs, in steps of 128; 0 = no rows
-  const int end0 = min(tok0 + p.tile_tokens, len), end1 = min(tok0 + span, len);
-  const int n0 = (end0 + kRows - 1) / kRows;
-  const int n1 = end1 > tok0 + p.tile_tokens ? (end1 + kRows - 1) / kRows : 0;
-  const int nmax = max(n0, n1);
-  const bool fix = nmax * kRows > len;       // the last step reaches behind the sequence
-
-  if (threadIdx.x == 0) {
-    for (int t = 0; t < 2; ++t) {
-      bar_init(bar_q + 8 * t, 1);
-      bar_init(bar_s + 8 * t, 1);
-      bar_init(bar_pa + 8 * t, 4);
-      bar_init(bar_p + 8 * t, 4);
-      bar_init(bar_o + 8 * t, 1);
-    }
-    bar_init(bar_fix, 1);
-    bar_init(bar_last, 1);
-    bar_init(bar_drain_mma, 1);
-    for (int i = 0; i < kPStages; ++i) {
-      bar_init(bar_full + 8 * i, 1);
-      bar_init(bar_empty + 8 * i, 1);
-    }
-    *abort = 0;
-    bar_init_fence();
+struct PromptWork {
+  static constexpr bool kBf16 = true, kPairs = false;
+  uint16_t* out;
+  float* lse;
+  float* part_o;
+  float2* part_ml;
+  int64_t out_stride;
+  int32_t group, n_q_heads, half_tokens;
+  float scale_log2;
+  Tiles<N> tiles;
+  ChunkCuts cuts;                            // n = 0: CTAs have whole tiles
+  __device__ __forceinline__ int first_slot() const { return cuts.n ? cuts.slot[blockIdx.x] : 0; }
+  __device__ __forceinline__ bool whole_tiles() const { return cuts.n == 0; }
+  __device__ __forceinline__ void whole(int tile, attend::Part& x) const {
+    const auto at = tiles.place(tile);
+    x.tile = tile;
+    x.len = at.len;
+    x.tok0 = at.tok0;
+    x.begin = 0;
+    x.items = x.end = steps_of(x.tok0, tiles.span, x.len);
+    x.causal0 = 0;
+    x.row0 = x.q_row = tiles.seqs.row[at.seq];
+    x.head0 = at.head * group;
+    x.kv = at.head;
+    x.slot = -1;
+    x.two = x.tok0 + half_tokens < x.len;
+    x.keep = static_cast<uint8_t>(min(kRows, x.len - (x.items - 1) * kRows));
   }
-  if (warp == 9) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
-  tmem_before();
-  __syncthreads();
-  tmem_after();
-  const uint32_t tmem = *tmem_slot;
-
-  if (warp < 8) {
-    more_regs<kPSoftRegs>();
-    const int t = warp >> 2;
-    const int n_t = t ? n1 : n0;
-    const uint32_t lanes = tmem + (static_cast<uint32_t>(warp & 3) << 21);
-    const uint32_t s_tm = lanes + t * kRows, o_tm = lanes + 256 + t * kRows;
-    const int r = (warp & 3) * 32 + lane;
-    const int tok_in = r / p.group;
-    const int pos = tok0 + t * p.tile_tokens + tok_in;
-    const bool real = tok_in < p.tile_tokens && pos < len;
-    const int first_pos = tok0 + t * p.tile_tokens + (warp & 3) * 32 / p.group;      // of the warp's rows
-    const float c = p.scale_log2;
-    float m = 0.f, l = 0.f;
-    bool ok = true;
-    for (int j = 0; j < n_t; ++j) {
-      if (!bar_wait(bar_s + 8 * t, j & 1, abort)) {
-        ok = false;
-        break;
-      }
-      tmem_after();
-      uint32_t x[kRows];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld32(s_tm + 32 * i, x + 32 * i);
-      tmem_wait_ld();
-      if ((j + 1) * kRows - 1 > first_pos) {
-        const int limit = pos - j * kRows;
-#pragma unroll
-        for (int i = 0; i < kRows; ++i)
-          if (i > limit) x[i] = 0xff800000u;
-      }
-      float mx[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) mx[k] = max3(__uint_as_float(x[3 * k]), __uint_as_float(x[3 * k + 1]), __uint_as_float(x[3 * k + 2]));
-#pragma unroll
-      for (int i = 12; i < kRows; i += 8)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (i + 2 * k < kRows) mx[k] = max3(mx[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
-      const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
-      if (j == 0) {
-        m = top == -INFINITY ? 0.f : top;
-      } else {
-        const bool move = (top - m) * c > kSlack;
-        if (__any_sync(0xffffffffu, move)) {
-          const float f = move ? ex2((m - top) * c) : 1.f;
-          m = move ? top : m;
-          l *= f;
-          const uint64_t ff = f2_pack(f, f);
-          for (int i = 0; i < 4; ++i) {
-            uint32_t o[32];
-            tmem_ld32(o_tm + 32 * i, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              float a, b;
-              f2_unpack(f2_mul(f2_pack(__uint_as_float(o[k]), __uint_as_float(o[k + 1])), ff), a, b);
-              o[k] = __float_as_uint(a);
-              o[k + 1] = __float_as_uint(b);
-            }
-            tmem_st32(o_tm + 32 * i, o);
-          }
-        }
-      }
-      const uint64_t cc = f2_pack(c, c), mm = f2_pack(-m * c, -m * c);
-      uint64_t sum0 = 0, sum1 = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t pk[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          float a, b;
-          f2_unpack(f2_fma(f2_pack(__uint_as_float(x[32 * i + 2 * k]), __uint_as_float(x[32 * i + 2 * k + 1])), cc, mm), a, b);
-          a = ex2(a);
-          b = ex2(b);
-          if (k & 1) sum1 = f2_add(sum1, f2_pack(a, b));
-          else sum0 = f2_add(sum0, f2_pack(a, b));
-          pk[k] = bf16_pair(a, b);
-        }
-        tmem_st16(s_tm + 16 * i, pk);
-        if (i == 2) {                        // three quarters of the weights: their product starts while the rest are made
-          tmem_wait_st();
-          tmem_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(bar_pa + 8 * t);
-        }
-      }
-      float a, b;
-      f2_unpack(f2_add(sum0, sum1), a, b);
-      l += a + b;
-      tmem_wait_st();
-      tmem_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(bar_p + 8 * t);
-    }
-    if (n_t > 0) {
-      ok = ok && bar_wait(bar_o + 8 * t, 0, abort);
-      tmem_after();
-      const float inv = ok ? 1.f / l : NAN;
-      const int hq = head * p.group + r % p.group;
-      uint16_t* dst = p.out + static_cast<int64_t>(row0 + pos) * p.out_stride + hq * kD;
-      for (int i = 0; i < 4; ++i) {
-        uint32_t o[32];
-        tmem_ld32(o_tm + 32 * i, o);
-        tmem_wait_ld();
-        if (real) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint4 v;
-            v.x = bf16_pair(__uint_as_float(o[8 * k]) * inv, __uint_as_float(o[8 * k + 1]) * inv);
-            v.y = bf16_pair(__uint_as_float(o[8 * k + 2]) * inv, __uint_as_float(o[8 * k + 3]) * inv);
-            v.z = bf16_pair(__uint_as_float(o[8 * k + 4]) * inv, __uint_as_float(o[8 * k + 5]) * inv);
-            v.w = bf16_pair(__uint_as_float(o[8 * k + 6]) * inv, __uint_as_float(o[8 * k + 7]) * inv);
-            *reinterpret_cast<uint4*>(dst + 32 * i + 8 * k) = v;
-          }
-        }
-      }
-      if (real && p.lse) p.lse[static_cast<int64_t>(row0 + pos) * p.n_q_heads + hq] = ok ? (m * c + lg2(l)) * kLn2 : NAN;
-    }
-  } else {
-    fewer_regs<kPOtherRegs>();
-    if (warp == 8) {
-      if (elect()) {
-        const uint32_t q_bytes = 2u * p.tile_tokens * p.group * 128u;
-        for (int t = 0; t < (n1 ? 2 : 1); ++t) {
-          bar_expect(bar_q + 8 * t, q_bytes);
-          for (int h = 0; h < 2; ++h)
-            tma_load_3d(smem + t * kTileBytes + h * kPanel, &map_q, 64 * h, head * p.group, row0 + tok0 + t * p.tile_tokens, bar_q + 8 * t);
-        }
-        int i = 0;
-        for (; i < 2 * nmax; ++i) {
-          const int slot = i % kPStages, turn = i / kPStages;
-          if (turn > 0 && !bar_wait(bar_empty + 8 * slot, (turn - 1) & 1, abort)) break;
-          bar_expect(bar_full + 8 * slot, kTileBytes);
-          const uint32_t dst = smem + kPOffStage + slot * kTileBytes;
-          for (int h = 0; h < 2; ++h)
-            tma_load_3d(dst + h * kPanel, i & 1 ? &map_v : &map_k, 64 * h, head, row0 + (i >> 1) * kRows, bar_full + 8 * slot);
-        }
-        if (*abort) {                        // what is on its way arrives before the CTA leaves
-          for (int t = 0; t < (n1 ? 2 : 1); ++t) bar_drain(bar_q + 8 * t, 0);
-          for (int k = max(0, i - kPStages); k < i; ++k) bar_drain(bar_full + 8 * (k % kPStages), (k / kPStages) & 1);
-        }
-      }
-    } else if (warp == 9) {
-      if (elect()) {
-        constexpr uint32_t id_qk = instr_desc(true, false, kRows, kRows), id_pv = instr_desc(true, true, kRows, kD);
-        auto wait_stage = [&](int i) { return bar_wait(bar_full + 8 * (i % kPStages), (i / kPStages) & 1, abort); };
-        auto free_stage = [&](int i) { mma_commit(bar_empty + 8 * (i % kPStages)); };
-        auto qk = [&](int t, int i) {
-          const uint64_t a = smem_desc(smem + t * kTileBytes, 16), b = smem_desc(smem + kPOffStage + (i % kPStages) * kTileBytes, 16);
-          for (int k = 0; k < kD / 16; ++k) {
-            const uint32_t off = ((k >> 2) * kPanel + (k & 3) * 32) >> 4;
-            mma_ss(tmem + t * kRows, a + off, b + off, id_qk, k > 0);
-          }
-          mma_commit(bar_s + 8 * t);
-        };
-        auto pv = [&](int t, int i, bool first, int from, int to) {
-          const uint64_t b = smem_desc(smem + kPOffStage + (i % kPStages) * kTileBytes, kPanel);
-          for (int k = from; k < to; ++k) mma_ts(tmem + 256 + t * kRows, tmem + t * kRows + 8 * k, b + ((k * 16 * 128) >> 4), id_pv, !first || k > 0);
-        };
-        bool ok = bar_wait(bar_q, 0, abort) && wait_stage(0);
-        if (ok) {
-          tmem_after();
-          qk(0, 0);
-          if (n1) {
-            ok = bar_wait(bar_q + 8, 0, abort);
-            if (ok) qk(1, 0);
-          }
-          free_stage(0);
-        }
-        for (int j = 0; ok && j < nmax; ++j) {
-          const int v = 2 * j + 1, k = 2 * j + 2;
-          ok = wait_stage(v) && (j + 1 == nmax || wait_stage(k));
-          if (ok && fix && j + 1 == nmax) {      // the last values are there: warp 10 zeroes the rows behind the sequence
-            bar_arrive(bar_last);
-            ok = bar_wait(bar_fix, 0, abort);
-          }
-          if (!ok) break;
-          for (int t = 0; t < 2 && ok; ++t) {
-            const int n_t = t ? n1 : n0;
-            if (j < n_t) {
-              ok = bar_wait(bar_pa + 8 * t, j & 1, abort);
-              if (!ok) break;
-              tmem_after();
-              pv(t, v, j == 0, 0, 6);
-              ok = bar_wait(bar_p + 8 * t, j & 1, abort);
-              if (!ok) break;
-              tmem_after();
-              pv(t, v, j == 0, 6, 8);
-              if (j + 1 == n_t) mma_commit(bar_o + 8 * t);
-              else qk(t, k);
-            }
-          }
-          free_stage(v);
-          if (j + 1 < nmax) free_stage(k);
-        }
-        if (!ok) {                           // products in flight end before tensor memory is given back
-          mma_commit(bar_drain_mma);
-          bar_drain(bar_drain_mma, 0);
-        }
-      }
-    } else if (warp == 10 && fix) {
-      if (bar_wait(bar_last, 0, abort)) {
-        const uint32_t v = smem + kPOffStage + (2 * nmax - 1) % kPStages * kTileBytes;
-        for (int k = (len - (nmax - 1) * kRows) * 8 + lane; k < kRows * 8; k += 32) {
-          sts128(v + k * 16, make_uint4(0, 0, 0, 0));
-          sts128(v + kPanel + k * 16, make_uint4(0, 0, 0, 0));
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) bar_arrive(bar_fix);
-      }
-    }
+  __device__ __forceinline__ bool next(int& state, int& slot, attend::Part& x) const {
+    const int tile = cuts.tile[blockIdx.x] + state, t1 = cuts.tile[blockIdx.x + 1], i1 = cuts.item[blockIdx.x + 1];
+    if (tile >= tiles.count() || tile > t1 || (tile == t1 && i1 == 0)) return false;
+    whole(tile, x);
+    if (state == 0) x.begin = cuts.item[blockIdx.x];
+    if (tile == t1) x.end = i1;
+    if (chunk_needs_slot(x.begin, x.end, x.items)) x.slot = slot++;
+    ++state;
+    return true;
   }
-  __syncwarp();
-  tmem_before();
-  __syncthreads();
-  if (warp == 9) tmem_dealloc(tmem, 512);
-}
+  __device__ __forceinline__ void load_q(const CUtensorMap* map, uint32_t dst, const attend::Part& x, int t, uint32_t bar) const {
+    for (int k = 0; k < 2; ++k) tma_load_3d(dst + k * kPanel, map, 64 * k, x.head0, x.q_row + x.tok0 + t * half_tokens, bar);
+  }
+  __device__ __forceinline__ void load_keys(const CUtensorMap* map, uint32_t dst, const attend::Part& x, int step, uint32_t bar) const {
+    tma_load_4d(dst, map, 0, x.kv, x.q_row + step * kRows, 0, bar);
+  }
+  __device__ __forceinline__ int flags(const attend::Part&, int) const { return 0; }
+  __device__ __forceinline__ const float* term(const attend::Part&, int) const { return nullptr; }
+  struct Where {
+    int tok0, len, head0;
+    int64_t row0;
+  };
+  __device__ __forceinline__ Where place(int tile) const {
+    const auto at = tiles.place(tile);
+    return {at.tok0, at.len, at.head * group, tiles.seqs.row[at.seq]};
+  }
+  __device__ __forceinline__ void fail() const {}      // (the rows without a result are NaN)
+};
 
 // ---- masses of prompt tokens ---------------------------------------------------------------------
 constexpr int kMThreads = 192;             // four warps of tokens, loads, products
@@ -524,7 +309,8 @@ __global__ void __launch_bounds__(kMThreads)
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-std::atomic<uint64_t> g_prompt_few{0}, g_prompt_many{0}, g_mass_few{0}, g_mass_many{0};
+std::atomic<uint64_t> g_mass_few{0}, g_mass_many{0};
+constexpr int kCutGain = 8, kCutSteps = 3;      // steps: see cut_prompt; what a CTA is worth starting for
 
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
@@ -572,15 +358,54 @@ std::vector<int> longest_first(const gkv_prompt* d) {
   return order;
 }
 
+// Cuts the launch's tiles into equal ranges where the longest one would outlast the rest by more than the parts' merge costs (about the
+// time of eight steps: one sequence of 4,097 tokens, 8 heads: 65 us whole, 33 steps for the last tile and 16.5 on average).  Returns the slots, 0 = whole tiles.
 template <int N>
-cudaError_t launch_prompt(PromptParams& p, const gkv_prompt* d, const std::vector<int>& order, int begin, int end, const CUtensorMap* maps, std::atomic<uint64_t>& done,
-                          cudaStream_t st) {
-  Seqs<N> s;
-  const int items = deal(s, d->offsets, order, begin, end, 2 * p.tile_tokens);
-  cudaError_t e = raise_smem_limit(prompt_kernel<N>, kPSmem, done);
+int cut_prompt(const Tiles<N>& t, ChunkCuts* cuts, ChunkMerge* merge) {
+  int64_t total = 0;
+  int longest = 0;
+  for (int i = 0; i < t.seqs.n; ++i)
+    for (int k = t.seqs.first[i]; k < t.seqs.first[i + 1]; ++k) {
+      const int n = steps_of((t.seqs.first[i + 1] - 1 - k) * t.span, t.span, t.seqs.len[i]);
+      total += static_cast<int64_t>(n + attend::kStart) * t.n_kv_heads;
+      longest = std::max(longest, n + attend::kStart);
+    }
+  cuts->n = 0;
+  merge->n = 0;
+  merge->slot[0] = 0;
+  if (longest <= total / kChunkCtas + kCutGain) return 0;
+  int seq = 0;
+  return cut_tiles(t.count(), total, kCutSteps, attend::kStart, attend::kSnap, [&](int tile) {
+    const int item = tile / t.n_kv_heads;
+    if (item < t.seqs.first[seq]) seq = 0;
+    while (item >= t.seqs.first[seq + 1]) ++seq;
+    return steps_of((t.seqs.first[seq + 1] - 1 - item) * t.span, t.span, t.seqs.len[seq]);
+  }, cuts, merge);
+}
+constexpr size_t slot_bytes_of_prompt(int slots) { return static_cast<size_t>(slots) * 2 * kRows * (kD + 2) * sizeof(float); }
+
+template <int N>
+void set_tiles(Tiles<N>& t, const gkv_prompt* d, const std::vector<int>& order, int begin, int end) {
+  t.n_kv_heads = d->n_kv_heads;
+  t.span = 2 * (kRows / (d->n_q_heads / d->n_kv_heads));
+  deal(t.seqs, d->offsets, order, begin, end, t.span);
+}
+
+template <int N>
+cudaError_t launch_prompt(PromptWork<N>& w, const gkv_prompt* d, const std::vector<int>& order, int begin, int end, const attend::Maps& maps, void* workspace,
+                          size_t bytes, cudaStream_t st) {
+  set_tiles(w.tiles, d, order, begin, end);
+  ChunkMerge merge;
+  const int slots = cut_prompt(w.tiles, &w.cuts, &merge);
+  if (slot_bytes_of_prompt(slots) > bytes || (slots && !workspace)) w.cuts.n = merge.n = 0;      // whole tiles then
+  w.part_o = static_cast<float*>(workspace);
+  w.part_ml = reinterpret_cast<float2*>(w.part_o + static_cast<size_t>(slots) * 2 * kRows * kD);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = raise_smem_limit(attend::attend_kernel<PromptWork<N>>, attend::kSmem, done);
   if (e != cudaSuccess) return e;
-  prompt_kernel<N><<<items * p.n_kv_heads, kPThreads, kPSmem, st>>>(p, s, maps[0], maps[1], maps[2]);
-  return cudaGetLastError();
+  attend::attend_kernel<PromptWork<N>><<<w.cuts.n ? w.cuts.n : w.tiles.count(), attend::kThreads, attend::kSmem, st>>>(w, maps);
+  if ((e = cudaGetLastError()) != cudaSuccess || merge.n == 0) return e;
+  return attend::launch_behind(attend::attend_merge_kernel<PromptWork<N>>, dim3((w.tiles.span * w.group + 31) / 32, merge.n), 128, 0, st, w, merge);
 }
 template <int N>
 cudaError_t launch_mass(MassParams& p, const gkv_prompt* d, const std::vector<int>& order, int begin, int end, const CUtensorMap* maps, size_t smem,
@@ -599,84 +424,90 @@ cudaError_t launch_mass(MassParams& p, const gkv_prompt* d, const std::vector<in
 float scale_of(const gkv_prompt* d) { return (d->softmax_scale > 0.f ? d->softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(kD)))) * kLog2e; }
 
 }  // namespace
-
-// Device memory of the current device (or memory that every device reaches): the kernels must not be given another GPU's.
-bool on_current_device(std::initializer_list<const void*> ptrs) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  for (const void* p : ptrs) {
-    if (!p) continue;
-    cudaPointerAttributes a{};
-    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-      cudaGetLastError();
-      return false;
-    }
-    if (a.type != cudaMemoryTypeManaged && (a.type != cudaMemoryTypeDevice || a.device != dev)) return false;
-  }
-  return true;
-}
-
-// A map of 16-bit elements with the 128-byte swizzle; strides of all dimensions but the first, in bytes.
-bool make_map(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
-  using Encode = decltype(&cuTensorMapEncodeTiled);
-  static const Encode encode = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found{};
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
-    return reinterpret_cast<Encode>(f);
-  }();
-  if (!encode) return false;
-  cuuint64_t d[5], s[4];
-  cuuint32_t b[5], step[5];
-  for (int i = 0; i < n; ++i) {
-    d[i] = dims[i];
-    b[i] = box[i];
-    step[i] = 1;
-    if (i) s[i - 1] = strides[i - 1];
-  }
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n, const_cast<void*>(base), d, s, b, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 }  // namespace gkv
 
 using namespace gkv;
 
-int gkv_prompt_attn(const gkv_prompt* d, const void* q, const void* k, const void* v, void* out, float* lse, void* stream) {
+namespace {
+// No exception leaves a C entry point: the sequences' order is the only memory that the calls take from the host.
+template <class F>
+int guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return GKV_ERR_INVALID_ARG;
+  }
+}
+
+int workspace_bytes_of(const gkv_prompt* d, size_t* bytes) {
+  int rows = 0;
+  const int rc = check_prompt(d, &rows);
+  if (rc != GKV_OK) return rc;
+  if (!bytes) return GKV_ERR_INVALID_ARG;
+  *bytes = 0;
+  const std::vector<int> order = longest_first(d);
+  const int n = static_cast<int>(order.size());
+  for (int at = 0; at < n; at += kMaxSeqs) {
+    const int end = std::min(n, at + kMaxSeqs);
+    ChunkCuts cuts;
+    ChunkMerge merge;
+    int slots;
+    if (end - at <= kFewSeqs) {
+      Tiles<kFewSeqs> t;
+      set_tiles(t, d, order, at, end);
+      slots = cut_prompt(t, &cuts, &merge);
+    } else {
+      Tiles<kMaxSeqs> t;
+      set_tiles(t, d, order, at, end);
+      slots = cut_prompt(t, &cuts, &merge);
+    }
+    *bytes = std::max(*bytes, slot_bytes_of_prompt(slots));
+  }
+  return GKV_OK;
+}
+
+int attn(const gkv_prompt* d, const void* q, const void* k, const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   int rows = 0;
   const int rc = check_prompt(d, &rows);
   if (rc != GKV_OK) return rc;
   const std::vector<int> order = longest_first(d);
   if (order.empty()) return GKV_OK;
-  if (!q || !k || !v || !out || misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16) || misaligned(lse, 4)) return GKV_ERR_INVALID_ARG;
-  if (!on_current_device({q, k, v, out, lse})) return GKV_ERR_INVALID_ARG;
+  if (!q || !k || !v || !out || misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16) || misaligned(lse, 4) || misaligned(workspace, 16))
+    return GKV_ERR_INVALID_ARG;
+  if (!on_current_device({q, k, v, out, lse, workspace})) return GKV_ERR_INVALID_ARG;
   const int64_t nq = static_cast<int64_t>(d->n_q_heads) * kD, nkv = static_cast<int64_t>(d->n_kv_heads) * kD;
-  PromptParams p{};
-  p.out = static_cast<uint16_t*>(out);
-  p.lse = lse;
-  p.out_stride = d->out_stride ? d->out_stride : nq;
-  p.n_q_heads = d->n_q_heads;
-  p.n_kv_heads = d->n_kv_heads;
-  p.group = d->n_q_heads / d->n_kv_heads;
-  p.tile_tokens = kRows / p.group;
-  p.scale_log2 = scale_of(d);
-  CUtensorMap maps[3];
-  if (!make_rows_map(&maps[0], q, rows, d->n_q_heads, d->q_stride ? d->q_stride : nq, p.group, p.tile_tokens) ||
-      !make_rows_map(&maps[1], k, rows, d->n_kv_heads, d->k_stride ? d->k_stride : nkv, 1, kRows) ||
-      !make_rows_map(&maps[2], v, rows, d->n_kv_heads, d->v_stride ? d->v_stride : nkv, 1, kRows))
+  const int group = d->n_q_heads / d->n_kv_heads, half_tokens = kRows / group;
+  attend::Maps maps;
+  // keys and values: [rows][heads][two panels][64 channels], 128 rows of a head at a time
+  const uint64_t dims[4] = {64, static_cast<uint64_t>(d->n_kv_heads), static_cast<uint64_t>(rows), 2};
+  const uint64_t ks[3] = {kRowBytes, static_cast<uint64_t>(d->k_stride ? d->k_stride : nkv) * 2, 128}, vs[3] = {kRowBytes, static_cast<uint64_t>(d->v_stride ? d->v_stride : nkv) * 2, 128};
+  const uint32_t box[4] = {64, 1, kRows, 2};
+  if (!make_rows_map(&maps.q, q, rows, d->n_q_heads, d->q_stride ? d->q_stride : nq, group, half_tokens) || !make_map(&maps.k, k, 4, dims, ks, box) ||
+      !make_map(&maps.v, v, 4, dims, vs, box))
     return GKV_ERR_CUDA;
+  maps.k_lo = maps.k;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto launch = [&](auto& w, int at, int end) {
+    w.out = static_cast<uint16_t*>(out);
+    w.lse = lse;
+    w.out_stride = d->out_stride ? d->out_stride : nq;
+    w.group = group;
+    w.n_q_heads = d->n_q_heads;
+    w.half_tokens = half_tokens;
+    w.scale_log2 = scale_of(d);
+    return launch_prompt(w, d, order, at, end, maps, workspace, workspace_bytes, st);
+  };
   const int n = static_cast<int>(order.size());
   for (int at = 0; at < n; at += kMaxSeqs) {
     const int end = std::min(n, at + kMaxSeqs);
-    const cudaError_t e = end - at <= kFewSeqs ? launch_prompt<kFewSeqs>(p, d, order, at, end, maps, g_prompt_few, st)
-                                               : launch_prompt<kMaxSeqs>(p, d, order, at, end, maps, g_prompt_many, st);
-    if (e != cudaSuccess) return GKV_ERR_CUDA;
+    PromptWork<kFewSeqs> few;
+    PromptWork<kMaxSeqs> many;
+    if ((end - at <= kFewSeqs ? launch(few, at, end) : launch(many, at, end)) != cudaSuccess) return GKV_ERR_CUDA;
   }
   return GKV_OK;
 }
 
-int gkv_prompt_mass(const gkv_prompt* d, const void* q, const void* k, const float* lse, int32_t n_obs, float* mass, void* stream) {
+int mass_of(const gkv_prompt* d, const void* q, const void* k, const float* lse, int32_t n_obs, float* mass, void* stream) {
   int rows = 0;
   const int rc = check_prompt(d, &rows);
   if (rc != GKV_OK) return rc;
@@ -714,4 +545,16 @@ int gkv_prompt_mass(const gkv_prompt* d, const void* q, const void* k, const flo
     if (e != cudaSuccess) return GKV_ERR_CUDA;
   }
   return GKV_OK;
+}
+}  // namespace
+
+int gkv_prompt_workspace_bytes(const gkv_prompt* d, size_t* bytes) {
+  return guarded([&] { return workspace_bytes_of(d, bytes); });
+}
+int gkv_prompt_attn(const gkv_prompt* d, const void* q, const void* k, const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  return guarded([&] { return attn(d, q, k, v, out, lse, workspace, workspace_bytes, stream); });
+}
+int gkv_prompt_mass(const gkv_prompt* d, const void* q, const void* k, const float* lse, int32_t n_obs, float* mass, void* stream) {
+  return guarded([&] { return mass_of(d, q, k, lse, n_obs, mass, stream); });
 }

@@ -14,12 +14,14 @@
 #include <stdint.h>
 
 namespace gkv {
-bool make_map(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+// A tensor map of 16-bit elements with the 128-byte swizzle; strides of all dimensions but the first, in bytes.  gkv_api.cu sets it when the library is
+// loaded: the files with kernels need nothing of the driver to link.
+inline bool (*make_map)(CUtensorMap* map, const void* base, int n, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) = nullptr;
 
 namespace tc {
 
-constexpr int kSpins = 1 << 20;            // failed polls after which a wait gives up
-constexpr uint32_t kHintNs = 1000;         // what one poll may sleep
+constexpr int kSpins = 1 << 20;            // failed polls after which a wait gives up (a poll sleeps as long as the hardware likes; with a hint of
+                                           // 1 us waits that lasted 300 cycles took up to 1000)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -39,11 +41,11 @@ __device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
       "selp.u32 %0, 1, 0, p;\n"
       "}\n"
       : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(kHintNs)
+      : "r"(bar), "r"(parity)
       : "memory");
   return ok != 0;
 }
@@ -82,10 +84,38 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
 // programmatic stream serialisation: what follows may be launched / what came before is done and visible
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+// ---- cluster launch control: a CTA of this grid that has not been launched yet is called off, and its work done here ----
+__device__ __forceinline__ void call_off(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];\n" ::"r"(answer), "r"(bar) : "memory");
+}
+// The answer (16 bytes, 16-byte aligned): was there one, and which
+__device__ __forceinline__ bool called_off(uint32_t answer, uint32_t& cta) {
+  uint32_t x, ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b128 r;\n"
+      "ld.shared.b128 r, [%2];\n"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+      "selp.u32 %1, 1, 0, p;\n"
+      "mov.u32 %0, 0;\n"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n"
+      "}\n"
+      : "=&r"(x), "=r"(ok)
+      : "r"(answer)
+      : "memory");
+  if (ok) cta = x;
+  return ok != 0;
+}
 // one lane of a converged warp
 __device__ __forceinline__ bool elect() {
   uint32_t ok;
@@ -160,6 +190,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
         "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),
         "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
       : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+                 "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+               : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
   asm volatile(

@@ -16,10 +16,10 @@ HARNESS = r"""
 #include "gkv_chunk.h"
 using namespace gkv;
 
-static int check(const ChunkShape& s, const int32_t* len, int min_items) {
+static int check(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap) {
   ChunkCuts cuts;
   ChunkMerge merge;
-  const int slots = chunk_plan(s, len, min_items, &cuts, &merge);
+  const int slots = chunk_plan(s, len, min_items, start, snap, &cuts, &merge);
   const int tiles = s.batch * s.n_kv_heads * s.row_tiles;
   if (s.tile_tokens * s.group > s.tile_rows || s.tile_tokens < 1 || s.row_tiles * s.tile_tokens < s.n_new) return 1;
   long total = 0;
@@ -28,12 +28,16 @@ static int check(const ChunkShape& s, const int32_t* len, int min_items) {
   if (cuts.n < 1 || cuts.n > kChunkCtas || cuts.tile[cuts.n] != tiles || cuts.item[cuts.n] != 0) return 3;
   // the kernel's own walk over its segments
   std::vector<std::vector<int>> of(tiles);
-  long seen = 0, most = 0, least = 1L << 60;
+  long seen = 0, most = 0, least = 1L << 60, cost_all = 0;
+  for (int t = 0; t < tiles; ++t) {
+    const int n = chunk_items(s, chunk_len(s, len, t / s.row_tiles / s.n_kv_heads), t % s.row_tiles);
+    cost_all += n ? n + start : 0;
+  }
   int next_tile = 0, next_item = 0, slot_end = 0;
   for (int c = 0; c < cuts.n; ++c) {
     int slot = cuts.slot[c];
     if (slot != slot_end) return 4;
-    long mine = 0;
+    long mine = 0, cost = 0;
     for (int t = cuts.tile[c]; t <= cuts.tile[c + 1] && t < tiles; ++t) {
       const int items = chunk_items(s, chunk_len(s, len, t / s.row_tiles / s.n_kv_heads), t % s.row_tiles);
       const int begin = t == cuts.tile[c] ? cuts.item[c] : 0, end = t == cuts.tile[c + 1] ? cuts.item[c + 1] : items;
@@ -43,14 +47,18 @@ static int check(const ChunkShape& s, const int32_t* len, int min_items) {
       if (t != next_tile || begin != next_item) return 6;
       next_item = end;
       mine += end - begin;
+      cost += end - begin + start;
       if (chunk_needs_slot(begin, end, items)) of[t].push_back(slot++);
     }
     slot_end = slot;
     seen += mine;
+    if (mine == 0) return 12;
+    // equal to within the beginning of a part, a step, and what cuts were moved by
+    if (cost > cost_all / std::min<long>(kChunkCtas, std::max(1L, cost_all / min_items)) + start + 1 + 2 * snap) return 13;
     most = std::max(most, mine);
     least = std::min(least, mine);
   }
-  if (seen != total || most - least > 1) return 7;
+  if (seen != total || (start == 0 && snap == 0 && most - least > 1)) return 7;
   if (slot_end != slots || slots > kChunkParts || slots > tiles + kChunkCtas - 1) return 8;
   int m = 0;
   for (int t = 0; t < tiles; ++t) {
@@ -77,7 +85,7 @@ int main() {
     std::vector<int32_t> len(s.batch);
     for (auto& n : len) n = upto(3) ? upto(s.n_new) : 0;
     for (const int32_t* l : {static_cast<const int32_t*>(nullptr), static_cast<const int32_t*>(len.data())})
-      if (const int rc = check(s, l, 1 + upto(8))) {
+      if (const int rc = check(s, l, 1 + upto(8), upto(1) * 2, upto(1))) {
         std::printf("case %d: %d (batch %d kv %d group %d new %d closed %d)\n", i, rc, s.batch, s.n_kv_heads, s.group, s.n_new, n_closed);
         return 1;
       }
