@@ -4,7 +4,8 @@
 // Attention: attend_kernel (gkv_attend.cuh) over tiles of the packed sequences, bf16 operands as they lie.
 //
 // mass_kernel.  S^T = K Q^T for the observing rows: a thread owns a token, so the sum over rows of exp2(c S - lse) needs no
-// exchange, and every sum has a fixed order.  K is read once.
+// exchange, and every sum has a fixed order.  K is read once.  Few rows: K's bytes (57,000 tokens of 8 heads with 64 rows: 25 us for 116 MB,
+// 0.70 of the copy's rate); many: 16 exponentials a cycle and SM (16,384 tokens of 2 heads with 512 rows: 15 us, 4 of them exponentials).
 //
 // Values of a sequence have to be finite; what lies behind a sequence's end may hold anything: its logits are masked by
 // selection and its value rows are zeroed in shared memory before they are used.
@@ -133,11 +134,14 @@ struct PromptWork {
 
 // ---- masses of prompt tokens ---------------------------------------------------------------------
 constexpr int kMThreads = 192;             // four warps of tokens, loads, products
-constexpr int kMStages = 2;
-constexpr int kMOffLse = kMStages * kTileBytes;
-constexpr int kMOffBar = kMOffLse + 256 * 4;
-constexpr int kMOffQ = kMOffBar + 1024;
-constexpr int kMaxObsRows = 256;           // rows of one product: its n dimension
+constexpr int kMaxObsRows = 128;           // rows of one product: its n dimension
+constexpr int kMOffLse = 0, kMOffBar = kMaxObsRows * 4, kMOffTiles = 1024;
+constexpr int kMCtas = 2;                  // resident on an SM
+// One product per tile: two tiles of keys, the rows once.  Several: one tile of keys, the rows twice.  Either way 97 KB at most.
+__host__ __device__ constexpr int mass_k_stages(bool one) { return one ? 2 : 1; }
+__host__ __device__ constexpr int mass_q_stages(bool one) { return one ? 1 : 2; }
+constexpr int mass_smem(bool one, int n_pad) { return kMOffTiles + mass_k_stages(one) * kTileBytes + mass_q_stages(one) * n_pad * 256 + 1024; }
+static_assert(kMCtas * (std::max(mass_smem(true, kMaxObsRows), mass_smem(false, kMaxObsRows)) + 1024) <= 227 * 1024, "two CTAs on an SM");
 
 struct MassParams {
   const float* lse;
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(kMThreads)
   uint8_t* const base = smem_raw + (smem - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t bars = smem + kMOffBar;
-  const uint32_t bar_q = bars, bar_qfree = bars + 8, bar_s = bars + 16, bar_sfree = bars + 32, bar_full = bars + 48, bar_empty = bars + 64, bar_drain_mma = bars + 80;
+  const uint32_t bar_q = bars, bar_qfree = bars + 16, bar_s = bars + 32, bar_sfree = bars + 48, bar_full = bars + 64, bar_empty = bars + 80, bar_drain_mma = bars + 96;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kMOffBar + 240);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kMOffBar + 244);
   float* const lse_s = reinterpret_cast<float*>(base + kMOffLse);
@@ -173,11 +177,14 @@ __global__ void __launch_bounds__(kMThreads)
   const int obs = min(p.n_obs, len), obs0 = len - obs;         // observing tokens, the first of them
   const int n_groups = (obs + p.group_tokens - 1) / p.group_tokens;
   const int steps = n_tiles * n_groups;
+  const bool one = p.n_obs <= p.group_tokens;                  // the launch's layout: a product holds all rows
+  const int k_stages = mass_k_stages(one), q_stages = mass_q_stages(one);
+  const uint32_t tiles = smem + kMOffTiles, q_smem = tiles + k_stages * kTileBytes;
 
   if (threadIdx.x == 0) {
-    bar_init(bar_q, 1);
-    bar_init(bar_qfree, 1);
     for (int i = 0; i < 2; ++i) {
+      bar_init(bar_q + 8 * i, 1);
+      bar_init(bar_qfree + 8 * i, 1);
       bar_init(bar_s + 8 * i, 1);
       bar_init(bar_sfree + 8 * i, 4);
       bar_init(bar_full + 8 * i, 1);
@@ -198,15 +205,21 @@ __global__ void __launch_bounds__(kMThreads)
     const int r = warp * 32 + lane;
     float sum = 0.f;
     bool ok = true;
+    // what a product's row gets, a thread per row, loaded a product ahead
+    auto row_lse = [&](int grp) {
+      const int q0 = obs0 + grp * p.group_tokens, cols = min(p.group_tokens, obs - grp * p.group_tokens) * p.group;
+      return r < cols ? -kLog2e * p.lse[static_cast<int64_t>(row0 + q0 + r / p.group) * p.n_q_heads + head * p.group + r % p.group] : 0.f;
+    };
+    float next = row_lse(0);
     for (int i = 0; i < steps; ++i) {
       const int grp = i % n_groups, tok = (tile0 + i / n_groups) * kRows + r;
       const int q0 = obs0 + grp * p.group_tokens;                                  // first observing token of the product
       const int cols = min(p.group_tokens, obs - grp * p.group_tokens) * p.group;
       if (i == 0 || n_groups > 1) {
         asm volatile("bar.sync 1, 128;\n" ::: "memory");
-        for (int k = r; k < cols; k += 128)
-          lse_s[k] = -kLog2e * p.lse[static_cast<int64_t>(row0 + q0 + k / p.group) * p.n_q_heads + head * p.group + k % p.group];
+        lse_s[r] = next;
         asm volatile("bar.sync 1, 128;\n" ::: "memory");
+        next = row_lse((grp + 1) % n_groups);
       }
       // (after an abort the loop goes on without products: its barriers need all four warps)
       ok = ok && bar_wait(bar_s + 8 * (i & 1), (i >> 1) & 1, abort);
@@ -257,26 +270,27 @@ __global__ void __launch_bounds__(kMThreads)
       for (; ok && i < steps; ++i) {
         const int grp = i % n_groups, tile = i / n_groups;
         if (grp == 0) {
-          const int slot = tile % kMStages, turn = tile / kMStages;
+          const int slot = tile % k_stages, turn = tile / k_stages;
           ok = turn == 0 || bar_wait(bar_empty + 8 * slot, (turn - 1) & 1, abort);
           if (!ok) break;
           bar_expect(bar_full + 8 * slot, kTileBytes);
           for (int h = 0; h < 2; ++h)
-            tma_load_3d(smem + slot * kTileBytes + h * kPanel, &map_k, 64 * h, head, row0 + (tile0 + tile) * kRows, bar_full + 8 * slot);
+            tma_load_3d(tiles + slot * kTileBytes + h * kPanel, &map_k, 64 * h, head, row0 + (tile0 + tile) * kRows, bar_full + 8 * slot);
           ++k_loads;
         }
         if (i == 0 || n_groups > 1) {
-          ok = i == 0 || bar_wait(bar_qfree, (i - 1) & 1, abort);
+          const int slot = i % q_stages, turn = i / q_stages;
+          ok = turn == 0 || bar_wait(bar_qfree + 8 * slot, (turn - 1) & 1, abort);
           if (!ok) break;
-          bar_expect(bar_q, q_bytes);
+          bar_expect(bar_q + 8 * slot, q_bytes);
           for (int h = 0; h < 2; ++h)
-            tma_load_3d(smem + kMOffQ + h * p.n_pad * 128, &map_q, 64 * h, head * p.group, row0 + obs0 + grp * p.group_tokens, bar_q);
+            tma_load_3d(q_smem + slot * p.n_pad * 256 + h * p.n_pad * 128, &map_q, 64 * h, head * p.group, row0 + obs0 + grp * p.group_tokens, bar_q + 8 * slot);
           ++q_loads;
         }
       }
       if (*abort) {
-        if (q_loads) bar_drain(bar_q, (q_loads - 1) & 1);
-        for (int k = max(0, k_loads - kMStages); k < k_loads; ++k) bar_drain(bar_full + 8 * (k % kMStages), (k / kMStages) & 1);
+        for (int k = max(0, q_loads - q_stages); k < q_loads; ++k) bar_drain(bar_q + 8 * (k % q_stages), (k / q_stages) & 1);
+        for (int k = max(0, k_loads - k_stages); k < k_loads; ++k) bar_drain(bar_full + 8 * (k % k_stages), (k / k_stages) & 1);
       }
     }
   } else {
@@ -284,16 +298,16 @@ __global__ void __launch_bounds__(kMThreads)
       const uint32_t idesc = instr_desc(true, false, kRows, p.n_pad);
       bool ok = true;
       for (int i = 0; i < steps; ++i) {
-        const int grp = i % n_groups, tile = i / n_groups, slot = tile % kMStages;
-        ok = (grp > 0 || bar_wait(bar_full + 8 * slot, (tile / kMStages) & 1, abort)) &&
-             ((i > 0 && n_groups == 1) || bar_wait(bar_q, i & 1, abort)) && (i < 2 || bar_wait(bar_sfree + 8 * (i & 1), ((i >> 1) - 1) & 1, abort));
+        const int grp = i % n_groups, tile = i / n_groups, slot = tile % k_stages, q_slot = n_groups == 1 ? 0 : i % q_stages;
+        ok = (grp > 0 || bar_wait(bar_full + 8 * slot, (tile / k_stages) & 1, abort)) &&
+             ((i > 0 && n_groups == 1) || bar_wait(bar_q + 8 * q_slot, (i / q_stages) & 1, abort)) && (i < 2 || bar_wait(bar_sfree + 8 * (i & 1), ((i >> 1) - 1) & 1, abort));
         if (!ok) break;
         tmem_after();
-        const uint64_t a = smem_desc(smem + slot * kTileBytes, 16), b = smem_desc(smem + kMOffQ, 16);
+        const uint64_t a = smem_desc(tiles + slot * kTileBytes, 16), b = smem_desc(q_smem + q_slot * p.n_pad * 256, 16);
         for (int k = 0; k < kD / 16; ++k)
           mma_ss(tmem + (i & 1) * p.pitch, a + (((k >> 2) * kPanel + (k & 3) * 32) >> 4), b + (((k >> 2) * p.n_pad * 128 + (k & 3) * 32) >> 4), idesc, k > 0);
         mma_commit(bar_s + 8 * (i & 1));
-        if (n_groups > 1) mma_commit(bar_qfree);
+        if (n_groups > 1) mma_commit(bar_qfree + 8 * q_slot);
         if (grp + 1 == n_groups) mma_commit(bar_empty + 8 * slot);
       }
       if (!ok) {
@@ -412,10 +426,15 @@ cudaError_t launch_mass(MassParams& p, const gkv_prompt* d, const std::vector<in
                         std::atomic<uint64_t>& done, cudaStream_t st) {
   Seqs<N> s;
   const int tiles = deal(s, d->offsets, order, begin, end, kRows);
-  // a few CTAs per SM; beyond that a CTA takes more tiles and loads its queries once
-  p.chunk = std::max(1, std::min(8, tiles * p.n_kv_heads / (3 * 148)));
+  // One CTA per place on the GPU with a stretch of tiles each (its rows are loaded once); where sequences are too many for that, several waves.  (Three
+  // sequences of 57,000 tokens, 8 heads: 446 CTAs of eight tiles, 1.5 waves, took 28.8 us.)
+  constexpr int kPlaces = 148 * kMCtas;
+  const int all = tiles * p.n_kv_heads, even = (all + kPlaces - 1) / kPlaces;
+  p.chunk = even;
+  while (p.chunk <= even + even / 4 && deal(s, d->offsets, order, begin, end, kRows * p.chunk) * p.n_kv_heads > kPlaces) ++p.chunk;
+  if (p.chunk > even + even / 4) p.chunk = std::max(1, all / (4 * kPlaces));
   const int items = deal(s, d->offsets, order, begin, end, kRows * p.chunk);
-  cudaError_t e = raise_smem_limit(mass_kernel<N>, kMOffQ + kMaxObsRows * 256 + 1024, done);
+  cudaError_t e = raise_smem_limit(mass_kernel<N>, std::max(mass_smem(true, kMaxObsRows), mass_smem(false, kMaxObsRows)), done);
   if (e != cudaSuccess) return e;
   mass_kernel<N><<<items * p.n_kv_heads, kMThreads, smem, st>>>(p, s, maps[0], maps[1]);
   return cudaGetLastError();
@@ -535,7 +554,7 @@ int mass_of(const gkv_prompt* d, const void* q, const void* k, const float* lse,
   if (!make_rows_map(&maps[0], q, rows, d->n_q_heads, d->q_stride ? d->q_stride : nq, p.group, p.group_tokens) ||
       !make_rows_map(&maps[1], k, rows, d->n_kv_heads, d->k_stride ? d->k_stride : nkv, 1, kRows))
     return GKV_ERR_CUDA;
-  const size_t smem = kMOffQ + static_cast<size_t>(p.n_pad) * 256 + 1024;
+  const size_t smem = mass_smem(n_obs <= p.group_tokens, p.n_pad);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int n = static_cast<int>(order.size());
   for (int at = 0; at < n; at += kMaxSeqs) {
