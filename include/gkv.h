@@ -181,7 +181,7 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
  * everything the cache holds, as gkv_decode_attn reads it, and to the chunk's own exact rows 0 .. i.  The cache is not changed: rows that
  * are to stay are appended with gkv_append_demote afterwards.  It may be empty.  Grouped-query layout only (GKV_ERR_UNSUPPORTED with v_aliases_k).
  *   q      device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned
- *   k_new, v_new  device bf16 [batch][n_new][n_kv_heads][128], 16-byte aligned
+ *   k_new, v_new  device bf16 [batch][n_new][n_kv_heads][128], 16-byte aligned (values of real tokens finite)
  *   len    HOST int32 [batch], 0 .. n_new: real tokens of each sequence (the rest of its rows is neither read for a result nor
  *          written), read during the call only; or NULL = n_new everywhere.  At most 1024 sequences with lengths (GKV_ERR_UNSUPPORTED)
  *          (values within +-65504, the cache's exact rows too: rows become fp16 where there are many; larger ones are clamped there)
@@ -218,7 +218,8 @@ typedef struct gkv_prompt {
 
 /* Causal attention of every query head over the exact rows of its own sequence (Sec. 3.1, Eq. 1 before anything is demoted):
  * query row i attends to rows 0 .. i of its sequence.  The call is asynchronous and may be captured into a graph.
- *   q    device bf16 [rows][n_q_heads][128]      k, v  device bf16 [rows][n_kv_heads][128]      (16-byte aligned)
+ *   q    device bf16 [rows][n_q_heads][128]      k, v  device bf16 [rows][n_kv_heads][128]      (16-byte aligned; the values of a sequence finite,
+ *        also those of tokens that come after the row: they get the weight 0)
  *   out  device bf16 [rows][n_q_heads][128], 16-byte aligned (rounded once, from fp32 accumulators; weights enter the
  *        value product as bf16)
  *   lse  device fp32 [rows][n_q_heads], packed, natural-log sum of exp(logit), or NULL

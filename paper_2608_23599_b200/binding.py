@@ -240,6 +240,8 @@ def _rows(t, name, dtype, shape=None):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != 128)):
         raise ValueError(f"{name}: the heads of a row have to follow one another")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] * 128:
+        raise ValueError(f"{name}: rows that share memory")
     return t.stride(0) if t.shape[0] > 1 else t.shape[1] * 128
 
 
@@ -292,7 +294,7 @@ def _prompt_space(device, need):
 def gkv_prompt_attn(q, k, v, out, offsets, lse=None, softmax_scale=0.0):
     """Causal attention of packed prompts: q, out cuda bf16 [rows][n_q_heads][128], k, v cuda bf16 [rows][n_kv_heads][128]
     (rows may be slices of a fused projection), offsets: host row numbers, sequence s = rows [offsets[s], offsets[s + 1]);
-    lse: cuda fp32 [rows][n_q_heads] or None.  Rows of no sequence are left as they are."""
+    lse: cuda fp32 [rows][n_q_heads] or None.  Rows of no sequence are left as they are; a sequence's own values have to be finite."""
     rc = (_call or _loaded()).prompt_attn(q, k, v, out, offsets, lse, softmax_scale, _prompt_spaces)
     if rc is not NotImplemented and rc > 0:      # bytes of workspace
         rc = _call.prompt_attn(q, k, v, out, offsets, lse, softmax_scale, _prompt_space(q.device, rc))
@@ -413,7 +415,7 @@ class Cache:
         """Attention of n_new new tokens per sequence over the cache and, causally, over one another; the cache stays as it is.
         q, out: cuda bf16 [B][n_new][Hq][128]; k_new, v_new: cuda bf16 [B][n_new][Hkv][128]; lse: cuda fp32 [B][n_new][Hq] or
         None; lengths: host ints [B] (rows from there on are left as they are) or None; workspace: a cuda tensor of
-        gkv_chunk_workspace_bytes bytes, or None (one is taken from torch's allocator for the call)."""
+        gkv_chunk_workspace_bytes bytes, or None (one per stream is kept; a captured call has one of its graph's own)."""
         cfg = self.cfg
         ws, keep = (workspace, None) if workspace is not None else self._chunk_workspace(layer, q)
         if isinstance(ws, torch.Tensor):
@@ -459,6 +461,11 @@ class Cache:
         dev, handle = self.arena.device, self.stream_handle
         st = torch._C._cuda_getCurrentRawStream(dev.index) if handle is None else handle
         capturing = torch._C._cuda_isCurrentStreamCapturing()
+        if handle is not None and handle != torch._C._cuda_getCurrentRawStream(dev.index):
+            with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=dev)):
+                if torch._C._cuda_isCurrentStreamCapturing():
+                    raise ValueError("workspace: a call that is captured on a stream other than torch's has to bring its own")
+            capturing = False
         kept = None if capturing else self._chunk_spaces.get(st)
         if kept is None or kept[0][1] < need:
             with torch.cuda.device(dev):

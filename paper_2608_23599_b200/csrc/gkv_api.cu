@@ -2026,7 +2026,7 @@ bool few_rows(const gkv_cache* c, int32_t n_new) { return static_cast<int64_t>(n
 int dense_group(const ChunkShape& s, int n_closed, size_t bytes) {
   const size_t one = dense_bytes(s, n_closed, 1, nullptr);
   if (bytes < one) return 0;
-  int n = static_cast<int>(std::min<size_t>(s.batch, bytes / one + 1));
+  int n = static_cast<int>(std::min<size_t>({static_cast<size_t>(s.batch), bytes / one + 1, static_cast<size_t>(std::max(1, 65535 / s.n_kv_heads))}));      // (a launch's y dimension)
   while (n > 1 && dense_bytes(s, n_closed, n, nullptr) > bytes) --n;
   return n;
 }

@@ -221,6 +221,7 @@ bool shaped(const Rows& r, int64_t a, int64_t b, int64_t c, int64_t d = 0) {
 bool heads_together(const Rows& r, int64_t* step) {
   if (r.shape[0] == 0 || r.shape[1] == 0 || r.shape[2] != 128 || r.stride[2] != 1 || (r.shape[1] > 1 && r.stride[1] != 128)) return false;
   *step = r.shape[0] > 1 ? r.stride[0] : r.shape[1] * 128;
+  if (*step < r.shape[1] * 128) return false;      // (rows that share memory; 0 would mean packed rows)
   return true;
 }
 // a contiguous array of 32-bit integers (numpy's, as a rule)
