@@ -196,7 +196,7 @@ GKV_API int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const voi
                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace that a gkv_chunk_attn of n_new tokens over the present context of `layer` works best with.  Few rows (n_new times the
- * query heads of a KV head up to 64) need less than 20 MB.  More rows have the cache written out as fp16 rows first, 768 bytes per token and KV head: the
+ * query heads of a KV head up to 64) need so much, less than 20 MB (GKV_ERR_INVALID_ARG below).  More rows have the cache written out as fp16 rows first, 768 bytes per token and KV head: the
  * answer is what all sequences need, or a number of them at a time that stays below 1 GiB (at least one).  A smaller workspace is
  * taken as long as it holds one sequence, with as many sequences at a time as it holds (GKV_ERR_INVALID_ARG below that).  bytes: host out. */
 GKV_API int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t* bytes);

@@ -2022,6 +2022,10 @@ int dense_rows(const gkv_cache* c, const LayerState& L) {
   return most;
 }
 bool few_rows(const gkv_cache* c, int32_t n_new) { return static_cast<int64_t>(n_new) * c->group <= kVerifyRows; }
+// A slot per stream that is cut, and one more per cut
+size_t verify_bytes(const gkv_cache* c) {
+  return static_cast<size_t>(std::min<int64_t>(kChunkParts, static_cast<int64_t>(c->n_streams) + kChunkCtas - 1)) * kChunkSlotFloats * sizeof(float);
+}
 // Sequences that go into a workspace together; 0 where not even one does
 int dense_group(const ChunkShape& s, int n_closed, size_t bytes) {
   const size_t one = dense_bytes(s, n_closed, 1, nullptr);
@@ -2038,7 +2042,7 @@ int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t
   const LayerState& L = c->layers[layer];
   ChunkShape s = chunk_of(c, n_new);
   if (few_rows(c, n_new)) {
-    *bytes = static_cast<size_t>(std::min<int64_t>(kChunkParts, static_cast<int64_t>(c->n_streams) + kChunkCtas - 1)) * kChunkSlotFloats * sizeof(float);      // a cut adds a slot
+    *bytes = verify_bytes(c);
     return GKV_OK;
   }
   dense_shape(&s, dense_rows(c, L));
@@ -2086,8 +2090,8 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
     verify_shape(&call.shape, L.n_closed, L.n_tail, call.res_rows);
     ChunkCuts cuts;
     ChunkMerge merge;
-    const int slots = chunk_plan(call.shape, len, 6, 0, 0, &cuts, &merge);
-    if (slots > 0 && (!workspace || workspace_bytes < static_cast<size_t>(slots) * kChunkSlotFloats * sizeof(float))) return GKV_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < verify_bytes(c)) return GKV_ERR_INVALID_ARG;      // (whatever this call's cuts need)
+    chunk_plan(call.shape, len, verify_min_items(call.shape), 0, 0, verify_second(call.shape), &cuts, &merge);
     CK(c, launch_verify(call, cuts, merge, len, st));
     return GKV_OK;
   }

@@ -54,14 +54,13 @@ inline bool chunk_needs_slot(int begin, int end, int items) { return begin > 0 |
 
 // Cuts `tiles` tiles, tile t of items(t) steps (asked for in order), into ranges of equal cost, one per CTA: a tile costs its steps and `start` more for its
 // beginning, `total` in all.  A cut that would come within `snap` of a tile's beginning or end comes there: a tile that is not cut needs no slots.
-// min_items: what a CTA is worth starting for.  Returns the number of slots; 0 with cuts->n = 0 where there is nothing to do.
+// n_ctas: ranges, at most kChunkCtas.  Returns the number of slots; 0 with cuts->n = 0 where there is nothing to do.
 template <class Items>
-inline int cut_tiles(int tiles, int64_t total, int min_items, int start, int snap, Items items, ChunkCuts* cuts, ChunkMerge* merge) {
+inline int cut_tiles(int tiles, int64_t total, int n_ctas, int start, int snap, Items items, ChunkCuts* cuts, ChunkMerge* merge) {
   cuts->n = 0;
   merge->n = 0;
   merge->slot[0] = 0;
   if (total == 0) return 0;
-  const int n_ctas = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / min_items)));
   // where CTAs begin: at the first tile that has steps, then at every n_ctas-th of the cost, places that fall together counted once
   int64_t at = 0;
   int c = 1, last_tile = -1, last_item = 0;
@@ -100,17 +99,30 @@ inline int cut_tiles(int tiles, int64_t total, int min_items, int start, int sna
   return slots;
 }
 
-// Tiles in the order (sequence, KV head, row tile)
-inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap, ChunkCuts* cuts, ChunkMerge* merge) {
-  int64_t total = 0;
+// CTAs for so much work, where one is worth starting for min_items
+inline int chunk_ctas(int64_t total, int min_items) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / min_items))); }
+
+// Tiles in the order (sequence, KV head, row tile).  second: what a CTA's second tile costs it, in items.  Where all tiles have the same number of items and it
+// is cheaper, every tile gets the same number of CTAs and none has two.
+inline int chunk_plan(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap, int second, ChunkCuts* cuts, ChunkMerge* merge) {
+  int64_t total = 0, filled = 0;
+  int most = 0, least = INT32_MAX;
   for (int b = 0; b < s.batch; ++b) {
     const int n = chunk_len(s, len, b);
     for (int rt = 0; rt < s.row_tiles && rt * s.tile_tokens < n; ++rt) {
       const int items = chunk_items(s, n, rt);
-      if (items) total += static_cast<int64_t>(s.n_kv_heads) * (items + start);
+      total += static_cast<int64_t>(s.n_kv_heads) * (items + start);
+      filled += s.n_kv_heads;
+      most = std::max(most, items);
+      least = std::min(least, items);
     }
   }
-  return cut_tiles(s.batch * s.n_kv_heads * s.row_tiles, total, min_items, start, snap,
+  int n = chunk_ctas(total, min_items);
+  if (most == least && filled <= n) {
+    const int even = n - static_cast<int>(n % filled);
+    if ((total + even - 1) / even <= total / n + second) n = even;
+  }
+  return cut_tiles(s.batch * s.n_kv_heads * s.row_tiles, total, n, start, snap,
                    [&](int tile) { return chunk_items(s, chunk_len(s, len, tile / s.row_tiles / s.n_kv_heads), tile % s.row_tiles); }, cuts, merge);
 }
 
@@ -164,6 +176,14 @@ inline void verify_shape(ChunkShape* s, int n_closed, int n_tail, int res_rows) 
   s->item_keys = 32;
   s->cache_items = 2 * n_closed + (n_tail + 31) / 32 + (res_rows + 31) / 32;
 }
+constexpr int kVerifyWarps = 12;             // of a CTA; a team has one per 16 rows
+inline int verify_teams(const ChunkShape& s) { return kVerifyWarps / ((s.n_new * s.group + 15) / 16); }
+// An item for every team but one, so that what an even division adds still is one round (eight streams of 33 items, 20 rows: 12.8 us with 48 CTAs, 13.4 with
+// 88, 19.4 with 44, of which half had two streams)
+inline int verify_min_items(const ChunkShape& s) { return std::max(2, verify_teams(s) - 1); }
+// A second stream costs a CTA about 9500 cycles (queries, the teams' merge, slots), an item 6000 of a team's (sixteen streams of 8,200 tokens, 64 rows: 45 us
+// with nine CTAs each, 50 with 148 cut anywhere; 64 streams of 32,757 would lose an eighth of the CTAs)
+inline int verify_second(const ChunkShape& s) { return 3 * verify_teams(s) / 2; }
 
 // ---- chunks of many rows (gkv_dense.cu): a tile is 256 rows in two halves, an item 128 rows of keys; centroids have a row each ----
 inline void dense_shape(ChunkShape* s, int rows) {      // rows: of the stream that has most

@@ -439,7 +439,7 @@ cudaError_t launch_dense(const ChunkCall& call, int first, int seqs, const int32
   s.batch = seqs;
   ChunkCuts cuts;
   ChunkMerge merge;
-  const int slots = chunk_plan(s, len ? len + first : nullptr, 4, attend::kStart, attend::kSnap, &cuts, &merge);
+  const int slots = chunk_plan(s, len ? len + first : nullptr, 4, attend::kStart, attend::kSnap, attend::kStart, &cuts, &merge);
   if (cuts.n == 0) return cudaSuccess;
   DensePlaces at;
   dense_bytes(s, call.n_closed, seqs, &at);

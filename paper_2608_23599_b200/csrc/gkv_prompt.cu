@@ -389,7 +389,7 @@ int cut_prompt(const Tiles<N>& t, ChunkCuts* cuts, ChunkMerge* merge) {
   merge->slot[0] = 0;
   if (longest <= total / kChunkCtas + kCutGain) return 0;
   int seq = 0;
-  return cut_tiles(t.count(), total, kCutSteps, attend::kStart, attend::kSnap, [&](int tile) {
+  return cut_tiles(t.count(), total, chunk_ctas(total, kCutSteps), attend::kStart, attend::kSnap, [&](int tile) {
     const int item = tile / t.n_kv_heads;
     if (item < t.seqs.first[seq]) seq = 0;
     while (item >= t.seqs.first[seq + 1]) ++seq;

@@ -12,7 +12,12 @@
 // 424 cycles of the SM's warp-level tensor pipes.  Tiles of 128 rows on the fifth-generation tensor cores would need the same 512 cycles for
 // any number of rows and every value written to shared memory first: with up to 64 rows a kernel of that kind took 1.9 times as long.
 //
-// Work split.  gkv_chunk.h cuts the streams' items (half blocks: 32 tokens) into equal ranges, one per CTA.  The CTA's warps form teams of
+// What it measured: 64 streams of 32,757 tokens on mixed rungs, 20 rows, 203 us, 0.25 of the copy bandwidth: 6000 cycles for a warp's item of 106
+// MMAs and 830 other instructions, of which 25% are waits of dependent instructions on one another with three warps a scheduler, 42% issue slots used,
+// tensor pipes 30%.  More warps have no registers (68 accumulators and 16 logits each); unrolling the logits' loop by 2 and 4 took 1.06 and 1.10 times as
+// long (instruction cache), a rolled value loop the same.
+//
+// Work split.  gkv_chunk.h cuts the streams' items (half blocks: 32 tokens) into equal ranges, one per CTA, or every stream into the same number.  The CTA's warps form teams of
 // one warp per 16 rows; a team takes every n-th item of the range and streams it through a ring of its own.  The rings are filled with bulk copies by
 // one warp more, in which a lane walks the items of each team.  (The team's first warp needed 1400 cycles of 6100 per half block for that.)  Exact
 // rows come 16 at a time by tensor map, two panels of 64 channels with the 128-byte swizzle: copies row by row took 80 cycles each to issue.
@@ -30,7 +35,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kVWarps = 12;                // that compute
+constexpr int kVWarps = kVerifyWarps;      // that compute
 constexpr int kVThreads = kVWarps * 32 + 128;
 constexpr int kVLaunchRegs = 128, kVWarpRegs = 152, kVFillRegs = 56;
 static_assert(kVWarps / 4 * kVWarpRegs + kVFillRegs <= (kVWarps / 4 + 1) * kVLaunchRegs, "a split draws on the launch's registers");

@@ -16,10 +16,10 @@ HARNESS = r"""
 #include "gkv_chunk.h"
 using namespace gkv;
 
-static int check(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap) {
+static int check(const ChunkShape& s, const int32_t* len, int min_items, int start, int snap, int second) {
   ChunkCuts cuts;
   ChunkMerge merge;
-  const int slots = chunk_plan(s, len, min_items, start, snap, &cuts, &merge);
+  const int slots = chunk_plan(s, len, min_items, start, snap, second, &cuts, &merge);
   const int tiles = s.batch * s.n_kv_heads * s.row_tiles;
   if (s.tile_tokens * s.group > s.tile_rows || s.tile_tokens < 1 || s.row_tiles * s.tile_tokens < s.n_new) return 1;
   long total = 0;
@@ -54,7 +54,7 @@ static int check(const ChunkShape& s, const int32_t* len, int min_items, int sta
     seen += mine;
     if (mine == 0) return 12;
     // equal to within the beginning of a part, a step, and what cuts were moved by
-    if (cost > cost_all / std::min<long>(kChunkCtas, std::max(1L, cost_all / min_items)) + start + 1 + 2 * snap) return 13;
+    if (cost > cost_all / std::min<long>(kChunkCtas, std::max(1L, cost_all / min_items)) + start + 1 + 2 * snap + second) return 13;
     most = std::max(most, mine);
     least = std::min(least, mine);
   }
@@ -85,7 +85,7 @@ int main() {
     std::vector<int32_t> len(s.batch);
     for (auto& n : len) n = upto(3) ? upto(s.n_new) : 0;
     for (const int32_t* l : {static_cast<const int32_t*>(nullptr), static_cast<const int32_t*>(len.data())})
-      if (const int rc = check(s, l, 1 + upto(8), upto(1) * 2, upto(1))) {
+      if (const int rc = check(s, l, 1 + upto(8), upto(1) * 2, upto(1), upto(1) * upto(12))) {
         std::printf("case %d: %d (batch %d kv %d group %d new %d closed %d)\n", i, rc, s.batch, s.n_kv_heads, s.group, s.n_new, n_closed);
         return 1;
       }
