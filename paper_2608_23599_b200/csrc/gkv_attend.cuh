@@ -257,19 +257,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmem_ld32(o_tm + 32 * i, o + 32 * i);
       tmem_wait_ld();
-      if (real) {
 #pragma unroll
-        for (int k = 0; k < kD; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
-        if (to >= 0) {                         // channel after channel: a warp's 32 rows are 128 bytes
+      for (int k = 0; k < kD; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
+      if (to >= 0) {                           // channel after channel: a warp's 32 rows are 128 bytes
+        if (real) {
           float* dst = work.part_o + static_cast<size_t>(to) * kD * 2 * kRows + slot_row;
 #pragma unroll
           for (int k = 0; k < kD; ++k) dst[k * 2 * kRows] = __uint_as_float(o[k]);
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(work.out + row * work.out_stride + hq * kD);
+        }
+      } else {
+        // Four lanes exchange their rows' 16-byte pieces, so that 64 bytes of a row are stored at a time.  (Rows stored by a lane each kept the
+        // load and store unit busy for 4096 cycles, and the barriers of the other warps waited behind them.)
+        uint16_t* const mine = real ? work.out + row * work.out_stride + hq * kD : nullptr;
 #pragma unroll
-          for (int k = 0; k < kD / 8; ++k)
-            dst[k] = make_uint4(bf16_pair(__uint_as_float(o[8 * k]), __uint_as_float(o[8 * k + 1])), bf16_pair(__uint_as_float(o[8 * k + 2]), __uint_as_float(o[8 * k + 3])),
-                                bf16_pair(__uint_as_float(o[8 * k + 4]), __uint_as_float(o[8 * k + 5])), bf16_pair(__uint_as_float(o[8 * k + 6]), __uint_as_float(o[8 * k + 7])));
+        for (int n = 0; n < 4; ++n) {
+          uint32_t w[4][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[j][k] = bf16_pair(__uint_as_float(o[32 * n + 8 * j + 2 * k]), __uint_as_float(o[32 * n + 8 * j + 2 * k + 1]));
+#pragma unroll
+          for (int d = 1; d < 4; d <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (!(j & d))
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & d ? w[j][k] : w[j | d][k], d);
+                  if (lane & d) w[j][k] = got;
+                  else w[j | d][k] = got;
+                }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint4* const dst = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), (lane & 28) | j));
+            if (dst) dst[4 * n + (lane & 3)] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+          }
         }
       }
       if (real) {

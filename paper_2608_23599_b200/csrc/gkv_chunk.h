@@ -178,9 +178,8 @@ inline void verify_shape(ChunkShape* s, int n_closed, int n_tail, int res_rows) 
 }
 constexpr int kVerifyWarps = 12;             // of a CTA; a team has one per 16 rows
 inline int verify_teams(const ChunkShape& s) { return kVerifyWarps / ((s.n_new * s.group + 15) / 16); }
-// An item for every team but one, so that what an even division adds still is one round (eight streams of 33 items, 20 rows: 12.8 us with 48 CTAs, 13.4 with
-// 88, 19.4 with 44, of which half had two streams)
-inline int verify_min_items(const ChunkShape& s) { return std::max(2, verify_teams(s) - 1); }
+// (two streams of 33 items, 16 rows, twelve teams: 12.8 us with 12 CTAs, 13.4 with 6, 22 and 32, 19.4 with 11, of which one had two streams)
+inline int verify_min_items(const ChunkShape& s) { return std::max(2, verify_teams(s) / 2 - 1); }
 // A second stream costs a CTA about 9500 cycles (queries, the teams' merge, slots), an item 6000 of a team's (sixteen streams of 8,200 tokens, 64 rows: 45 us
 // with nine CTAs each, 50 with 148 cut anywhere; 64 streams of 32,757 would lose an eighth of the CTAs)
 inline int verify_second(const ChunkShape& s) { return 3 * verify_teams(s) / 2; }
