@@ -13,14 +13,15 @@
 //
 // What bounds it: a half's chain of a step is 216 cycles to the maximum, 1490 for 128 exponentials a thread (1024 of the special-function unit), 400 until the
 // product is issued and 1160 for the rest of P V and Q K, 3010 in all for 2048 cycles of matrix products of both halves; 16,384 tokens of 16
-// query heads reach 1.34 PFLOP/s, 0.97 of what cuBLAS sustains under the power limit.  Evaluating a share of the exponentials by a polynomial on
+// query heads take 826 us, 1.33 PFLOP/s, ten times in a row, and 951 over seconds under the power limit (0.83 of what cuBLAS sustains there).  Evaluating a share of the exponentials by a polynomial on
 // the FMA pipe gained nothing (1/8 and 1/4 of them: 0.99 and 0.97 of the rate): the clock falls by what the pipes gain.
 //
 // Work split.  One CTA per SM.  Either all tiles' steps are laid end to end and cut into equal ranges, one per CTA (gkv_chunk.h), and a tile that was cut
 // leaves partial results in slots; or, where no tile is long enough for that to pay, a CTA has a whole tile and goes on
 // with those of CTAs that have not been launched yet (cluster launch control), heaviest first.  A warp works out the
 // CTA's parts ahead of the others (1250 cycles each, as much for constant memory as for arithmetic), and the next part's queries and keys are on
-// their way while the results of this one are written (a tile as a CTA of its own: 5300 cycles to the first logits, 6600 behind the last).
+// their way while the results of this one are written.  A part costs 8,000 to 10,000 cycles beside its steps: its halves begin together and share the
+// exponentials (the first step takes 5400), the last products end (2500), the rows leave (2600).
 #pragma once
 #include <cuda_runtime.h>
 

