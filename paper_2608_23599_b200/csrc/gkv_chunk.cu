@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
   float top = -INFINITY;
   for (int i = lane; i < n; i += 32) {
     const float2 v = p.part_ml[index(i)];
-    if (v.y > 0.f) top = fmaxf(top, v.x);
+    if (v.y != 0.f) top = fmaxf(top, v.x);      // (NaN counts: it has to come through)
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if (i0 + k >= n || !(v[k].y > 0.f)) continue;
+      if (i0 + k >= n || v[k].y == 0.f) continue;
       const float f = ex2(v[k].x - top);
       sum += f * v[k].y;
       o.x += f * x[k].x;

@@ -729,10 +729,10 @@ __global__ void __launch_bounds__(kVThreads, 1)
     for (int i = warp; i < rows; i += kVWarps) {           // a warp per row, four channels per lane; lane t has team t's factor
       const int at0 = (i >> 4) * 16 + (i & 15), step = p.groups * 16;
       const float2 v = lane < lay.teams ? mml[at0 + lane * step] : make_float2(0.f, 0.f);
-      float top = v.y > 0.f ? v.x : -INFINITY;
+      float top = v.y != 0.f ? v.x : -INFINITY;      // (NaN counts: it has to come through)
 #pragma unroll
       for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));      // (at most 12 teams)
-      const float f = v.y > 0.f ? ex2(v.x - top) : 0.f;
+      const float f = v.y != 0.f ? ex2(v.x - top) : 0.f;
       float sum = f * v.y;
 #pragma unroll
       for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);

@@ -210,6 +210,31 @@ def test_keys_of_later_new_tokens_may_be_anything(n_new):
     assert torch.equal(out[:, :-2], o2[:, :-2]) and torch.equal(lse[:, :-2], l2[:, :-2])
 
 
+@pytest.mark.parametrize("n_new", [6, 70])
+@pytest.mark.parametrize("ctx", [0, 64 * 40 + 9])
+def test_a_broken_key_is_seen(n_new, ctx):
+    """NaN comes through to every row that sees it, also where one of a stream's parts has it and the others have not."""
+    c, oc, g = tc.caches(8, 2, ctx, seed=38, plan=4 if ctx else None, **EXT)
+    q, k, v = tc.chunk(g, 1, n_new, 8, 2)
+    out, lse = tc.run(c, q, k, v)
+    bad = k.clone()
+    bad[:, 3, :, 5] = math.nan
+    o2, l2 = tc.run(c, q, bad, v)
+    assert torch.equal(out[:, :3], o2[:, :3]) and torch.equal(lse[:, :3], l2[:, :3])
+    assert bool(o2[:, 3:].isnan().all()) and bool(l2[:, 3:].isnan().all())
+
+
+@pytest.mark.parametrize("n", [300, 2500])
+def test_a_broken_key_of_a_prompt_is_seen(n):
+    q, k, v, off = tp.make([n], 8, 2, seed=39)
+    out, lse = tp.run(q, k, v, off)
+    bad = k.clone()
+    bad[100, :, 5] = math.nan
+    o2, l2 = tp.run(q, bad, v, off)
+    assert torch.equal(out[:100], o2[:100]) and torch.equal(lse[:100], l2[:100])
+    assert bool(o2[100:].isnan().all()) and bool(l2[100:].isnan().all())
+
+
 # ---- together ----
 @pytest.mark.parametrize("turn", [5, 150])
 def test_prompt_in_pieces(turn):
