@@ -251,8 +251,23 @@ def _floats(t, name, n, shape=None):
         raise ValueError(f"{name}: a contiguous CUDA float32 tensor {list(shape) if shape is not None else [n]} is needed")
 
 
+def _ints(x, name):
+    a = np.asarray(x)
+    if a.size and (a.dtype.kind not in "iu" or a.min() < -2 ** 31 or a.max() >= 2 ** 31):
+        raise ValueError(f"{name}: whole numbers of 32 bits are needed")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def _keep_space(spaces, key, kept):
+    """Keeps a stream's workspace, of at most four streams (the memory of the oldest goes back to torch's allocator, in the order of its stream)."""
+    spaces.pop(key, None)
+    while len(spaces) >= 4:
+        spaces.pop(next(iter(spaces)))
+    spaces[key] = kept
+
+
 def _prompt(q, k, offsets, softmax_scale, *more):
-    off = np.ascontiguousarray(offsets, dtype=np.int32)
+    off = _ints(offsets, "offsets")
     if off.ndim != 1 or off.size < 1:
         raise ValueError("offsets: n_seqs + 1 row numbers are needed")
     if off[-1] > q.shape[0]:
@@ -287,7 +302,7 @@ def _prompt_space(device, need):
             t = torch.empty(need, dtype=torch.uint8, device=device)
             kept = t.data_ptr(), need, t
             if not captured:
-                _prompt_spaces[key] = kept
+                _keep_space(_prompt_spaces, key, kept)
     return kept
 
 
@@ -441,7 +456,7 @@ class Cache:
             raise ValueError(f"workspace: a contiguous tensor on {dev} is needed")
         ln = None
         if lengths is not None:
-            ln = np.ascontiguousarray(lengths, dtype=np.int32)
+            ln = _ints(lengths, "lengths")
             if ln.shape != (b,):
                 raise ValueError(f"lengths: {b} of them are needed")
 
@@ -476,7 +491,7 @@ class Cache:
                         t = torch.empty(need, dtype=torch.uint8, device=dev)
             kept = (t.data_ptr(), need), t
             if not capturing:
-                self._chunk_spaces[st] = kept
+                _keep_space(self._chunk_spaces, st, kept)
         return kept
 
     def gkv_debug_export_bounds(self, layer):

@@ -97,3 +97,17 @@ def test_tensors_of_the_wrong_kind():
         B.gkv_prompt_mass(q, k, torch.zeros(5, 8), torch.zeros(10), [0, 5], 16)
     with pytest.raises(ValueError, match="q: a CUDA"):
         B.gkv_prompt_attn(None, k, k, q, [0, 5])
+
+
+@pytest.mark.parametrize("bad", [[0, 5.5], np.array([0.0, 5.0]), [0, 2 ** 31], np.array([0, 2 ** 32 + 5]), ["0", "5"]])
+def test_row_numbers_have_to_be_whole_numbers_of_32_bits(bad):
+    with pytest.raises(ValueError, match="offsets: whole numbers"):
+        B._ints(bad, "offsets")
+    assert B._ints([0, 5], "x").dtype == B._ints([], "x").dtype == B._ints(torch.tensor([3]), "x").dtype == np.int32
+
+
+def test_workspaces_of_four_streams_are_kept():
+    spaces = {}
+    for stream in (1, 2, 3, 1, 4, 5, 6):
+        B._keep_space(spaces, stream, (stream, 0))
+    assert list(spaces) == [1, 4, 5, 6]
