@@ -68,12 +68,19 @@ struct Maps {
 // part_ml (slots: [128 channels][256 rows], [256 rows]), and on the device
 //   next(state, slot, part)              the CTA's next part; state (at first 0) and slot (at first first_slot()) are the walk's
 //   whole_tiles(), whole(tile, part)     CTAs have whole tiles, a CTA per tile launched; the tile of that number
+//   ln2_rest                             see lse_of
 //   load_q(map, dst, part, t, bar)       half t's queries (two panels of half_tokens * group rows)
 //   load_keys(map, dst, part, step, bar) a step's 128 rows (two panels)
 //   flags(part, step), term(part, step)  kPairs only
 //   place(tile)                          where a tile lies (tok0, len, row0, head0)
 //   fail()                               a wait was given up
 constexpr int kHasTerm = 1, kHasLow = 2;
+
+// The log-sum-exp of weights 2^(x - top) that sum to `sum`; ln2_rest: what a logit is more of itself than its 32 bits say
+template <class Work>
+__device__ __forceinline__ float lse_of(const Work& work, float top, float sum) {
+  return fmaf(top, kLn2, fmaf(top, work.ln2_rest, lg2(sum) * kLn2));
+}
 
 template <class Work>
 __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_constant__ Work work, const __grid_constant__ Maps maps) {
@@ -297,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       }
       if (real) {
         if (to >= 0) work.part_ml[static_cast<size_t>(to) * 2 * kRows + slot_row] = make_float2(m * c, ok ? l : NAN);
-        else if (work.lse) work.lse[row * work.n_q_heads + hq] = ok ? (m * c + lg2(l)) * kLn2 : NAN;
+        else if (work.lse) work.lse[row * work.n_q_heads + hq] = ok ? lse_of(work, m * c, l) : NAN;
       }
       tmem_before();
     }
@@ -513,7 +520,7 @@ __global__ void __launch_bounds__(128) attend_merge_kernel(const __grid_constant
     const int64_t line = at.row0 + at.tok0 + r / work.group;
     reinterpret_cast<uint2*>(work.out + line * work.out_stride + head * kD)[lane] = make_uint2(turn[i * 65 + 2 * lane], turn[i * 65 + 2 * lane + 1]);
   }
-  if (warp == 0 && row < rows && work.lse) work.lse[(at.row0 + at.tok0 + row / work.group) * work.n_q_heads + at.head0 + row % work.group] = (top + lg2(sum)) * kLn2;
+  if (warp == 0 && row < rows && work.lse) work.lse[(at.row0 + at.tok0 + row / work.group) * work.n_q_heads + at.head0 + row % work.group] = lse_of(work, top, sum);
 }
 
 // Launched while the kernel in front is still running; `early`: that kernel lets this one in.

@@ -316,6 +316,7 @@ using attend::kHasTerm;
 template <int N>
 struct DenseWork {
   static constexpr bool kBf16 = false, kPairs = true;
+  static constexpr float ln2_rest = 0.f;
   uint16_t* out;
   float* lse;
   float* part_o;

@@ -5,7 +5,7 @@
 //
 // mass_kernel.  S^T = K Q^T for the observing rows: a thread owns a token, so the sum over rows of exp2(c S - lse) needs no
 // exchange, and every sum has a fixed order.  K is read once.  Few rows: K's bytes (57,000 tokens of 8 heads with 64 rows: 25 us for 116 MB,
-// 0.70 of the copy's rate); many: 16 exponentials a cycle and SM (16,384 tokens of 2 heads with 512 rows: 15 us, 4 of them exponentials).
+// 0.70 of the copy's rate); many: 16 exponentials a cycle and SM (16,384 tokens of 2 heads with 512 rows: 15.5 us, 4 of them exponentials).
 //
 // Values of a sequence have to be finite; what lies behind a sequence's end may hold anything: its logits are masked by
 // selection and its value rows are zeroed in shared memory before they are used.
@@ -83,7 +83,7 @@ struct PromptWork {
   float2* part_ml;
   int64_t out_stride;
   int32_t group, n_q_heads, half_tokens;
-  float scale_log2;
+  float scale_log2, ln2_rest;
   Tiles<N> tiles;
   ChunkCuts cuts;                            // n = 0: CTAs have whole tiles
   __device__ __forceinline__ int first_slot() const { return cuts.n ? cuts.slot[blockIdx.x] : 0; }
@@ -135,7 +135,7 @@ struct PromptWork {
 // ---- masses of prompt tokens ---------------------------------------------------------------------
 constexpr int kMThreads = 192;             // four warps of tokens, loads, products
 constexpr int kMaxObsRows = 128;           // rows of one product: its n dimension
-constexpr int kMOffLse = 0, kMOffBar = kMaxObsRows * 4, kMOffTiles = 1024;
+constexpr int kMOffLse = 0, kMOffBar = kMaxObsRows * 8, kMOffTiles = 2048;
 constexpr int kMCtas = 2;                  // resident on an SM
 // One product per tile: two tiles of keys, the rows once.  Several: one tile of keys, the rows twice.  Either way 97 KB at most.
 __host__ __device__ constexpr int mass_k_stages(bool one) { return one ? 2 : 1; }
@@ -152,7 +152,7 @@ struct MassParams {
   int32_t n_pad;                             // columns of a product, a multiple of 16
   int32_t pitch, tmem_cols;                  // the same rounded up to what one load reads; two of them
   int32_t chunk;                             // tiles of 128 tokens per CTA
-  float scale_log2;
+  float scale_log2, scale_rest;              // what a logit is multiplied by, in two parts (see logit_of)
 };
 
 template <int N>
@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(kMThreads)
   const uint32_t bar_q = bars, bar_qfree = bars + 16, bar_s = bars + 32, bar_sfree = bars + 48, bar_full = bars + 64, bar_empty = bars + 80, bar_drain_mma = bars + 96;
   volatile uint32_t* const abort = reinterpret_cast<volatile uint32_t*>(base + kMOffBar + 240);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kMOffBar + 244);
-  float* const lse_s = reinterpret_cast<float*>(base + kMOffLse);
+  float* const lse_s = reinterpret_cast<float*>(base + kMOffLse);      // what a row's logits get,
+  float* const by_s = lse_s + kMaxObsRows;                             // and what its weights are multiplied by
 
   const int head = blockIdx.x % p.n_kv_heads, item = blockIdx.x / p.n_kv_heads;
   const int si = find_seq(seqs, item);
@@ -205,10 +206,17 @@ __global__ void __launch_bounds__(kMThreads)
     const int r = warp * 32 + lane;
     float sum = 0.f;
     bool ok = true;
-    // what a product's row gets, a thread per row, loaded a product ahead
+    // a row's log-sum-exp, a thread per row, loaded a product ahead
     auto row_lse = [&](int grp) {
       const int q0 = obs0 + grp * p.group_tokens, cols = min(p.group_tokens, obs - grp * p.group_tokens) * p.group;
-      return r < cols ? -kLog2e * p.lse[static_cast<int64_t>(row0 + q0 + r / p.group) * p.n_q_heads + head * p.group + r % p.group] : 0.f;
+      return r < cols ? p.lse[static_cast<int64_t>(row0 + q0 + r / p.group) * p.n_q_heads + head * p.group + r % p.group] : 0.f;
+    };
+    const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), rest2 = f2_pack(p.scale_rest, p.scale_rest);
+    auto weights = [&](uint32_t s0, uint32_t s1, float e0, float e1) {      // of two rows
+      const uint64_t s = f2_pack(__uint_as_float(s0), __uint_as_float(s1));
+      float a, b;
+      f2_unpack(f2_fma(s, rest2, f2_fma(s, scale2, f2_pack(e0, e1))), a, b);
+      return f2_pack(ex2(a), ex2(b));
     };
     float next = row_lse(0);
     for (int i = 0; i < steps; ++i) {
@@ -217,7 +225,12 @@ __global__ void __launch_bounds__(kMThreads)
       const int cols = min(p.group_tokens, obs - grp * p.group_tokens) * p.group;
       if (i == 0 || n_groups > 1) {
         asm volatile("bar.sync 1, 128;\n" ::: "memory");
-        lse_s[r] = next;
+        // Its multiple of 32 bits would be off by up to 2^-20, as much as all else together: what is cut off goes into a factor.  (With the second part of
+        // the scale 1.4 us of 16,384 tokens' 16; errors of given log-sum-exps' masses 1.8e-6 -> 1.0e-6 and 2.2e-6 -> 1.6e-6 at logits of 12 and 25.)
+        constexpr float kRest = static_cast<float>(1.4426950408889634 - kLog2e);
+        const float e = -next * kLog2e;
+        lse_s[r] = e;
+        by_s[r] = fmaf(fmaf(-next, kLog2e, -e) - next * kRest, kLn2, 1.f);
         asm volatile("bar.sync 1, 128;\n" ::: "memory");
         next = row_lse((grp + 1) % n_groups);
       }
@@ -226,7 +239,7 @@ __global__ void __launch_bounds__(kMThreads)
       if (!ok) continue;
       tmem_after();
       const int from = max(0, (tok - q0) * p.group);           // rows before the token do not see it
-      float part0 = 0.f, part1 = 0.f;
+      uint64_t sum0 = 0, sum1 = 0;
       for (int c0 = 0; c0 < cols; c0 += 32) {
         uint32_t x[32];
         tmem_ld32(lanes + (i & 1) * p.pitch + c0, x);
@@ -234,18 +247,23 @@ __global__ void __launch_bounds__(kMThreads)
         if (c0 + 32 <= cols && __all_sync(0xffffffffu, from <= c0)) {
 #pragma unroll
           for (int k = 0; k < 32; k += 4) {
-            const float4 e = *reinterpret_cast<const float4*>(lse_s + c0 + k);
-            part0 += ex2(fmaf(__uint_as_float(x[k]), p.scale_log2, e.x)) + ex2(fmaf(__uint_as_float(x[k + 1]), p.scale_log2, e.y));
-            part1 += ex2(fmaf(__uint_as_float(x[k + 2]), p.scale_log2, e.z)) + ex2(fmaf(__uint_as_float(x[k + 3]), p.scale_log2, e.w));
+            const float4 e = *reinterpret_cast<const float4*>(lse_s + c0 + k), f = *reinterpret_cast<const float4*>(by_s + c0 + k);
+            sum0 = f2_fma(weights(x[k], x[k + 1], e.x, e.y), f2_pack(f.x, f.y), sum0);
+            sum1 = f2_fma(weights(x[k + 2], x[k + 3], e.z, e.w), f2_pack(f.z, f.w), sum1);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const float w = ex2(fmaf(__uint_as_float(x[k]), p.scale_log2, lse_s[c0 + k]));
-            part0 += c0 + k >= from && c0 + k < cols ? w : 0.f;
+          for (int k = 0; k < 32; k += 2) {
+            float a, b;
+            f2_unpack(f2_mul(weights(x[k], x[k + 1], lse_s[c0 + k], lse_s[c0 + k + 1]), f2_pack(by_s[c0 + k], by_s[c0 + k + 1])), a, b);
+            a = c0 + k >= from && c0 + k < cols ? a : 0.f;
+            b = c0 + k + 1 >= from && c0 + k + 1 < cols ? b : 0.f;
+            sum0 = f2_add(sum0, f2_pack(a, b));
           }
         }
       }
+      float part0, part1;
+      f2_unpack(f2_add(sum0, sum1), part0, part1);
       sum += part0 + part1;
       tmem_before();
       __syncwarp();
@@ -440,7 +458,12 @@ cudaError_t launch_mass(MassParams& p, const gkv_prompt* d, const std::vector<in
   return cudaGetLastError();
 }
 
-float scale_of(const gkv_prompt* d) { return (d->softmax_scale > 0.f ? d->softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(kD)))) * kLog2e; }
+double scale_of(const gkv_prompt* d) { return d->softmax_scale > 0.f ? d->softmax_scale : 1.0 / std::sqrt(static_cast<double>(kD)); }
+float scale_log2_of(const gkv_prompt* d) { return static_cast<float>(scale_of(d)) * kLog2e; }
+// What a logit is, in units of its multiple of scale_log2: ln 2, the rounding of scale_log2 taken out, and what tcgen05 loses.  It cuts sums instead
+// of rounding them: 128 products come out 7e-8 of themselves too small (6.9e-8 to 7.2e-8 for queries of unit variance times 3 and 6), which for
+// logits of 20 is more than all roundings together.
+double logit_of(const gkv_prompt* d) { return scale_of(d) / scale_log2_of(d) * (1.0 + 7e-8); }
 
 }  // namespace
 }  // namespace gkv
@@ -513,7 +536,8 @@ int attn(const gkv_prompt* d, const void* q, const void* k, const void* v, void*
     w.group = group;
     w.n_q_heads = d->n_q_heads;
     w.half_tokens = half_tokens;
-    w.scale_log2 = scale_of(d);
+    w.scale_log2 = scale_log2_of(d);
+    w.ln2_rest = static_cast<float>(logit_of(d) - kLn2);
     return launch_prompt(w, d, order, at, end, maps, workspace, workspace_bytes, st);
   };
   const int n = static_cast<int>(order.size());
@@ -549,7 +573,8 @@ int mass_of(const gkv_prompt* d, const void* q, const void* k, const float* lse,
   p.pitch = (p.n_pad + 31) / 32 * 32;
   p.tmem_cols = 64;
   while (p.tmem_cols < 2 * p.pitch) p.tmem_cols *= 2;
-  p.scale_log2 = scale_of(d);
+  p.scale_log2 = scale_log2_of(d);
+  p.scale_rest = static_cast<float>(p.scale_log2 * (logit_of(d) * 1.4426950408889634 - 1.0));
   CUtensorMap maps[2];
   if (!make_rows_map(&maps[0], q, rows, d->n_q_heads, d->q_stride ? d->q_stride : nq, p.group, p.group_tokens) ||
       !make_rows_map(&maps[1], k, rows, d->n_kv_heads, d->k_stride ? d->k_stride : nkv, 1, kRows))

@@ -1,5 +1,5 @@
 """How a chunk call's work is cut into CTAs, run on the host from the kernel's own header: every item of every tile is in exactly one
-range, ranges are equal to within one item, a tile's slots follow one another, and a call never needs more of them than its workspace holds."""
+range, ranges are equal to within one item (or what a tile's beginning counts for and cuts are moved by), a tile's slots follow one another, and a call never needs more of them than its workspace holds."""
 import os
 import shutil
 import subprocess
