@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(128) attend_merge_kernel(const __grid_constant
   if (warp == 0 && row < rows && work.lse) work.lse[(at.row0 + at.tok0 + row / work.group) * work.n_q_heads + at.head0 + row % work.group] = lse_of(work, top, sum);
 }
 
-// Launched while the kernel in front is still running; `early`: that kernel lets this one in.
+// Launched while the kernel in front is still running, which lets it in (pdl_launch) and which it waits for (pdl_wait)
 template <typename... Params, typename... Args>
 cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
