@@ -128,6 +128,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     prefetch_map(&maps.v);
   }
   if (warp == 9) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+  // the CTA's first part is worked out while tensor memory is allocated: it comes of the parameters alone
+  Part x;
+  int state = 0, slot = 0;
+  bool more = false;
+  if (warp == 11) {
+    slot = work.first_slot();
+    more = work.whole_tiles();
+    if (more) work.whole(blockIdx.x, x);
+    else more = work.next(state, slot, x);
+  }
   tmem_before();
   __syncthreads();
   tmem_after();
@@ -144,7 +154,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     return x.tile >= 0;
   };
   auto part_read = [&](int n) { bar_arrive(bar_got + 8 * (n % kParts)); };
-  Part x;
 
   if (warp < 8) {
     more_regs<kSoftRegs>();
@@ -444,27 +453,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     } else if (elect()) {
       // ---- the CTA's parts ----
       // Whole tiles: the CTA's own, then those of CTAs that have not been launched yet and are called off here (heaviest first, as they come)
-      int state = 0, slot = work.first_slot();
       const bool whole = work.whole_tiles();
       uint32_t tile = blockIdx.x;
       for (int n = 0;; ++n) {
-        bool more;
-        if (whole) {
-          more = n == 0;
-          if (n > 0) {
-            // not before the last step of the tile before is being loaded: a tile called off early is one that no idle CTA can have
-            if (!bar_wait(bar_more, (n - 1) & 1, abort)) break;
-            fence_async();
-            bar_expect(bar_call, 16);
-            call_off(answer, bar_call);
-            if (!bar_wait(bar_call, (n - 1) & 1, abort)) {
-              bar_drain(bar_call, (n - 1) & 1);
-              break;
-            }
-            more = called_off(answer, tile);
+        if (n > 0 && whole) {
+          // not before the last step of the tile before is being loaded: a tile called off early is one that no idle CTA can have
+          if (!bar_wait(bar_more, (n - 1) & 1, abort)) break;
+          fence_async();
+          bar_expect(bar_call, 16);
+          call_off(answer, bar_call);
+          if (!bar_wait(bar_call, (n - 1) & 1, abort)) {
+            bar_drain(bar_call, (n - 1) & 1);
+            break;
           }
+          more = called_off(answer, tile);
           if (more) work.whole(tile, x);
-        } else {
+        } else if (n > 0) {
           more = work.next(state, slot, x);
         }
         if (!more) x.tile = -1;
