@@ -127,7 +127,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
     prefetch_map(&maps.k);
     prefetch_map(&maps.v);
   }
-  if (warp == 9) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+  if (warp == 9) {                         // (no tensor memory is held while the kernel in front, which may still want some, is waited for)
+    pdl_wait();
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+  }
   // the CTA's first part is worked out while tensor memory is allocated: it comes of the parameters alone
   Part x;
   int state = 0, slot = 0;
@@ -491,6 +494,7 @@ __global__ void __launch_bounds__(128) attend_merge_kernel(const __grid_constant
   __shared__ uint32_t turn[32 * 65];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = merge.slot[blockIdx.y], n = merge.slot[blockIdx.y + 1] - first;
   const auto at = work.place(merge.tile[blockIdx.y]);
+  pdl_launch();
   const int row = blockIdx.x * 32 + lane, rows = min(2 * work.half_tokens, at.len - at.tok0) * work.group;
   if (blockIdx.x * 32 >= rows) return;
   pdl_wait();

@@ -24,6 +24,7 @@ struct MergeParams {
 template <int N>
 __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant__ MergeParams p, const __grid_constant__ ChunkMerge merge,
                                                           const __grid_constant__ ChunkLens<N> lens) {
+  pdl_launch();
   const ChunkShape& sh = p.s;
   const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int tile = merge.tile[blockIdx.y], first = merge.slot[blockIdx.y], n = merge.slot[blockIdx.y + 1] - first;

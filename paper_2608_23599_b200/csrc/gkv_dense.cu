@@ -66,6 +66,7 @@ __device__ __forceinline__ float half_of(uint32_t w, int i) { return __half2floa
 // CTAs [0, streams): a stream's blocks in order.  The others: queries as fp16 rows, and the steps' flags cleared.
 __global__ void __launch_bounds__(256) order_kernel(const __grid_constant__ DenseParams p, int streams, size_t pieces, size_t first) {
   pdl_launch();
+  pdl_wait();
   const int stream = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (stream >= streams) {
     const size_t i = static_cast<size_t>(blockIdx.x - streams) * 256 + tid;
@@ -485,13 +486,14 @@ cudaError_t launch_dense(const ChunkCall& call, int first, int seqs, const int32
     return cudaErrorInvalidValue;
   const size_t per_seq = static_cast<size_t>(s.n_new) * heads * kD / 8, pieces = per_seq * seqs;
   const size_t threads = std::max(pieces, static_cast<size_t>(streams) * p.steps);
-  order_kernel<<<static_cast<unsigned>(streams + (threads + 255) / 256), 256, 0, st>>>(p, streams, pieces, per_seq * first);
+  cudaError_t e = attend::launch_behind(order_kernel, dim3(static_cast<unsigned>(streams + (threads + 255) / 256)), 256, 0, st, p, streams, pieces, per_seq * first);
+  if (e != cudaSuccess) return e;
   const dim3 grid(2 * p.steps, streams);
   const bool one = !len || call.shape.batch == 1;
   ChunkLens<1> l1{{len ? len[0] : s.n_new}};
   ChunkLens<kChunkMaxBatch> ln;
   if (!one) std::copy(len, len + call.shape.batch, ln.len);
-  const cudaError_t e = one ? attend::launch_behind(expand_kernel<1>, grid, kEThreads, 0, st, p, l1) : attend::launch_behind(expand_kernel<kChunkMaxBatch>, grid, kEThreads, 0, st, p, ln);
+  e = one ? attend::launch_behind(expand_kernel<1>, grid, kEThreads, 0, st, p, l1) : attend::launch_behind(expand_kernel<kChunkMaxBatch>, grid, kEThreads, 0, st, p, ln);
   if (e != cudaSuccess) return e;
   return one ? launch_attend(p, maps, cuts, merge, l1, st) : launch_attend(p, maps, cuts, merge, ln, st);
 }

@@ -195,11 +195,16 @@ __global__ void __launch_bounds__(kMThreads)
     *abort = 0;
     bar_init_fence();
   }
-  if (warp == 5) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), p.tmem_cols);
+  if (warp == 5) {                         // (no tensor memory is held while the kernel in front, which may still want some, is waited for)
+    pdl_wait();
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), p.tmem_cols);
+  }
   tmem_before();
   __syncthreads();
   tmem_after();
   const uint32_t tmem = *tmem_slot;
+  pdl_launch();
+  pdl_wait();                              // (nothing but parameters was read so far)
 
   if (warp < 4) {
     const uint32_t lanes = tmem + (static_cast<uint32_t>(warp) << 21);
@@ -435,8 +440,8 @@ cudaError_t launch_prompt(PromptWork<N>& w, const gkv_prompt* d, const std::vect
   static std::atomic<uint64_t> done{0};
   cudaError_t e = raise_smem_limit(attend::attend_kernel<PromptWork<N>>, attend::kSmem, done);
   if (e != cudaSuccess) return e;
-  attend::attend_kernel<PromptWork<N>><<<w.cuts.n ? w.cuts.n : w.tiles.count(), attend::kThreads, attend::kSmem, st>>>(w, maps);
-  if ((e = cudaGetLastError()) != cudaSuccess || merge.n == 0) return e;
+  e = attend::launch_behind(attend::attend_kernel<PromptWork<N>>, dim3(w.cuts.n ? w.cuts.n : w.tiles.count()), attend::kThreads, attend::kSmem, st, w, maps);
+  if (e != cudaSuccess || merge.n == 0) return e;
   return attend::launch_behind(attend::attend_merge_kernel<PromptWork<N>>, dim3((w.tiles.span * w.group + 31) / 32, merge.n), 128, 0, st, w, merge);
 }
 template <int N>
@@ -454,8 +459,7 @@ cudaError_t launch_mass(MassParams& p, const gkv_prompt* d, const std::vector<in
   const int items = deal(s, d->offsets, order, begin, end, kRows * p.chunk);
   cudaError_t e = raise_smem_limit(mass_kernel<N>, std::max(mass_smem(true, kMaxObsRows), mass_smem(false, kMaxObsRows)), done);
   if (e != cudaSuccess) return e;
-  mass_kernel<N><<<items * p.n_kv_heads, kMThreads, smem, st>>>(p, s, maps[0], maps[1]);
-  return cudaGetLastError();
+  return attend::launch_behind(mass_kernel<N>, dim3(items * p.n_kv_heads), kMThreads, smem, st, p, s, maps[0], maps[1]);
 }
 
 double scale_of(const gkv_prompt* d) { return d->softmax_scale > 0.f ? d->softmax_scale : 1.0 / std::sqrt(static_cast<double>(kD)); }

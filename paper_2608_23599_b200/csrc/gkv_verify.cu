@@ -26,6 +26,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include "gkv_attend.cuh"
 #include "gkv_chunk.h"
 #include "gkv_internal.h"
 #include "gkv_tc.cuh"
@@ -368,6 +369,7 @@ __global__ void __launch_bounds__(kVThreads, 1)
   };
   Part x;
   pdl_launch();                            // (the merge waits for the whole grid; its blocks may take their places)
+  pdl_wait();                              // (nothing but parameters was read so far)
 
   if (warp >= kVWarps) {
     fewer_regs<kVFillRegs>();
@@ -771,8 +773,7 @@ cudaError_t launch_as(const VerifyParams& p, const VerifyMaps& maps, const Chunk
   for (int g = 1; g <= kVerifyRows / 16; ++g) most = std::max(most, static_cast<size_t>(verify_layout(g).bytes));
   const cudaError_t e = raise_smem_limit(verify_kernel<N>, most, done);
   if (e != cudaSuccess) return e;
-  verify_kernel<N><<<cuts.n, kVThreads, p.lay.bytes, st>>>(p, cuts, lens, maps);
-  return cudaGetLastError();
+  return attend::launch_behind(verify_kernel<N>, dim3(cuts.n), kVThreads, p.lay.bytes, st, p, cuts, lens, maps);
 }
 
 }  // namespace
