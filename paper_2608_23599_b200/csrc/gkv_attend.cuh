@@ -13,7 +13,7 @@
 //
 // What bounds it: a half's chain of a step is 216 cycles to the maximum, 1490 for 128 exponentials a thread (1024 of the special-function unit), 400 until the
 // product is issued and 1160 for the rest of P V and Q K, 3010 in all for 2048 cycles of matrix products of both halves; 16,384 tokens of 16
-// query heads take 826 us, 1.33 PFLOP/s, ten times in a row, and 951 over seconds under the power limit (0.83 of what cuBLAS sustains there).  Evaluating a share of the exponentials by a polynomial on
+// query heads take 815 us, 1.35 PFLOP/s, ten times in a row, and 957 over seconds under the power limit (0.83 of what cuBLAS sustains there).  Evaluating a share of the exponentials by a polynomial on
 // the FMA pipe gained nothing (1/8 and 1/4 of them: 0.99 and 0.97 of the rate): the clock falls by what the pipes gain.
 //
 // Work split.  One CTA per SM.  Either all tiles' steps are laid end to end and cut into equal ranges, one per CTA (gkv_chunk.h), and a tile that was cut

@@ -4,8 +4,8 @@
 // Attention: attend_kernel (gkv_attend.cuh) over tiles of the packed sequences, bf16 operands as they lie.
 //
 // mass_kernel.  S^T = K Q^T for the observing rows: a thread owns a token, so the sum over rows of exp2(c S - lse) needs no
-// exchange, and every sum has a fixed order.  K is read once.  Few rows: K's bytes (57,000 tokens of 8 heads with 64 rows: 25 us for 116 MB,
-// 0.70 of the copy's rate); many: 16 exponentials a cycle and SM (16,384 tokens of 2 heads with 512 rows: 15.5 us, 4 of them exponentials).
+// exchange, and every sum has a fixed order.  K is read once.  Few rows: K's bytes (57,000 tokens of 8 heads with 64 rows: 24.9 us for 116 MB,
+// 0.71 of the copy's rate); many: 16 exponentials a cycle and SM (16,384 tokens of 2 heads with 512 rows: 12.8 us, 4 of them exponentials).
 //
 // Values of a sequence have to be finite; what lies behind a sequence's end may hold anything: its logits are masked by
 // selection and its value rows are zeroed in shared memory before they are used.
@@ -396,7 +396,7 @@ std::vector<int> longest_first(const gkv_prompt* d) {
 }
 
 // Cuts the launch's tiles into equal ranges where the longest one would outlast the rest by more than the parts' merge costs (about the
-// time of eight steps: one sequence of 4,097 tokens, 8 heads: 65 us whole, 33 steps for the last tile and 16.5 on average, 56 cut).  Returns the slots, 0 = whole tiles.
+// time of eight steps: one sequence of 4,097 tokens, 8 heads: 65 us whole, 33 steps for the last tile and 16.5 on average, 54 cut).  Returns the slots, 0 = whole tiles.
 template <int N>
 int cut_prompt(const Tiles<N>& t, ChunkCuts* cuts, ChunkMerge* merge) {
   int64_t total = 0;

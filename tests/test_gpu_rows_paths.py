@@ -235,6 +235,41 @@ def test_a_broken_key_of_a_prompt_is_seen(n):
     assert bool(o2[100:].isnan().all()) and bool(l2[100:].isnan().all())
 
 
+def test_calls_in_a_row_into_the_same_buffers():
+    """Each kernel is launched while the one in front still runs: nothing is read or written before that one is done."""
+    sets = [tp.make([900, 33], 8, 2, seed=s) for s in (41, 42)]
+    off = sets[0][3]
+    alone = []
+    for q, k, v, _ in sets:
+        out, lse = tp.run(q, k, v, off)
+        mass = torch.zeros(933 * 2, device=DEV)
+        B.gkv_prompt_mass(q, k, lse, mass, off, 40)
+        alone.append((out, lse, mass))
+    c, oc, g = tc.caches(8, 2, 64 * 20 + 5, seed=43, plan=4, **EXT)
+    xs = [[t.to(DEV) for t in tc.chunk(g, 1, n, 8, 2)] for n in (6, 70, 6, 70)]
+    chunks = []
+    for x in xs:
+        out, lse = torch.zeros_like(x[0]), torch.zeros(x[0].shape[:3], device=DEV)
+        c.gkv_chunk_attn(0, *x, out, lse=lse)
+        torch.cuda.synchronize()
+        chunks.append((out, lse))
+    q, k, v = (torch.empty_like(t.contiguous()) for t in sets[0][:3])
+    out, lse, mass = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV), torch.empty(933 * 2, device=DEV)
+    co = {n: (torch.empty(1, n, 8, 128, dtype=torch.bfloat16, device=DEV), torch.empty(1, n, 8, device=DEV)) for n in (6, 70)}
+    for i in range(40):
+        for t, src in zip((q, k, v), sets[i % 2]):
+            t.copy_(src)
+        B.gkv_prompt_attn(q, k, v, out, off, lse=lse)
+        B.gkv_prompt_mass(q, k, lse, mass, off, 40)
+        got = [t.clone() for t in (out, lse, mass)]
+        x, n = xs[i % 4], xs[i % 4][0].shape[1]
+        c.gkv_chunk_attn(0, *x, *co[n][:1], lse=co[n][1])
+        c.gkv_chunk_attn(0, *xs[(i + 1) % 4], *co[76 - n][:1], lse=co[76 - n][1])
+        got += [t.clone() for t in (*co[n], *co[76 - n])]
+        for a, b in zip(got, (*alone[i % 2], *chunks[i % 4], *chunks[(i + 1) % 4])):
+            assert torch.equal(a, b), i
+
+
 # ---- together ----
 @pytest.mark.parametrize("turn", [5, 150])
 def test_prompt_in_pieces(turn):
