@@ -145,8 +145,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   __syncthreads();
   tmem_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_launch();
   pdl_wait();
+  pdl_launch();
   // The n-th part: false at the end, or after an abort.  Whoever has read it says so.
   auto part = [&](int n, Part& x) {
     if (!bar_wait(bar_put + 8 * (n % kParts), (n / kParts) & 1, abort)) return false;
@@ -494,10 +494,10 @@ __global__ void __launch_bounds__(128) attend_merge_kernel(const __grid_constant
   __shared__ uint32_t turn[32 * 65];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = merge.slot[blockIdx.y], n = merge.slot[blockIdx.y + 1] - first;
   const auto at = work.place(merge.tile[blockIdx.y]);
-  pdl_launch();
   const int row = blockIdx.x * 32 + lane, rows = min(2 * work.half_tokens, at.len - at.tok0) * work.group;
   if (blockIdx.x * 32 >= rows) return;
   pdl_wait();
+  pdl_launch();
   const float* const o0 = work.part_o + (static_cast<size_t>(first) * kD + 32 * warp) * 2 * kRows + row;
   const float2* const ml = work.part_ml + static_cast<size_t>(first) * 2 * kRows + row;
   float top = -INFINITY, sum = 0.f, o[32];

@@ -24,7 +24,6 @@ struct MergeParams {
 template <int N>
 __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant__ MergeParams p, const __grid_constant__ ChunkMerge merge,
                                                           const __grid_constant__ ChunkLens<N> lens) {
-  pdl_launch();
   const ChunkShape& sh = p.s;
   const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int tile = merge.tile[blockIdx.y], first = merge.slot[blockIdx.y], n = merge.slot[blockIdx.y + 1] - first;
@@ -32,6 +31,7 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
   const int tok = rt * sh.tile_tokens + row / sh.group;
   if (row >= sh.tile_tokens * sh.group || tok >= lens.len[N == 1 ? 0 : b]) return;
   pdl_wait();
+  pdl_launch();
   auto index = [&](int i) { return static_cast<size_t>(first + i) * sh.tile_rows + row; };
   float top = -INFINITY;
   for (int i = lane; i < n; i += 32) {

@@ -65,8 +65,8 @@ __device__ __forceinline__ float half_of(uint32_t w, int i) { return __half2floa
 
 // CTAs [0, streams): a stream's blocks in order.  The others: queries as fp16 rows, and the steps' flags cleared.
 __global__ void __launch_bounds__(256) order_kernel(const __grid_constant__ DenseParams p, int streams, size_t pieces, size_t first) {
-  pdl_launch();
   pdl_wait();
+  pdl_launch();
   const int stream = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (stream >= streams) {
     const size_t i = static_cast<size_t>(blockIdx.x - streams) * 256 + tid;
@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(kEThreads) expand_kernel(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const size_t row0 = static_cast<size_t>(stream) * p.stream_rows + static_cast<size_t>(unit) * kBlock;
   const int len = lens.len[N == 1 ? 0 : b];
-  pdl_launch();
   pdl_wait();
+  pdl_launch();
   const TableEntry* table = p.table + static_cast<size_t>(real) * p.table_stride;
   const TableEntry* order = p.order + static_cast<size_t>(stream) * p.n_closed;
   const int blocks = p.blocks[stream];

@@ -203,8 +203,8 @@ __global__ void __launch_bounds__(kMThreads)
   __syncthreads();
   tmem_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_launch();
   pdl_wait();                              // (nothing but parameters was read so far)
+  pdl_launch();
 
   if (warp < 4) {
     const uint32_t lanes = tmem + (static_cast<uint32_t>(warp) << 21);

@@ -89,7 +89,8 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-// programmatic stream serialisation: what follows may be launched / what came before is done and visible
+// programmatic stream serialisation: what follows may be launched / what came before is done and visible.  Kernels wait first and launch then: what
+// follows may do something before its own wait that the kernel before this one must not overlap.
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
 // ---- cluster launch control: a CTA of this grid that has not been launched yet is called off, and its work done here ----

@@ -368,8 +368,8 @@ __global__ void __launch_bounds__(kVThreads, 1)
     return false;
   };
   Part x;
-  pdl_launch();                            // (the merge waits for the whole grid; its blocks may take their places)
   pdl_wait();                              // (nothing but parameters was read so far)
+  pdl_launch();                            // (the merge waits for the whole grid; its blocks may take their places)
 
   if (warp >= kVWarps) {
     fewer_regs<kVFillRegs>();
