@@ -270,6 +270,34 @@ def test_calls_in_a_row_into_the_same_buffers():
             assert torch.equal(a, b), i
 
 
+def test_appends_chunks_and_reads_in_a_row():
+    """Blocks close and work lists are made anew between chunks and reads that are launched behind one another: as with a wait after each call."""
+    kw = dict(policy=B.POLICY_STAIRCASE, stair_tokens=(64, 128, 128, 64))
+    both = []
+    for waits in (True, False):
+        c, oc, g = tc.caches(8, 2, 64 * 9 + 50, batch=2, seed=44, max_ctx=2048, **kw)
+        new = [[t.to(DEV) for t in tc.chunk(g, 2, 6, 8, 2)] for _ in range(90)]
+        kept = []
+        torch.cuda.synchronize()
+        for q, k, v in new:
+            c.gkv_append_demote(0, k[:, :1].contiguous(), v[:, :1].contiguous())
+            steps = [torch.empty_like(q), torch.empty(2, 8, 128, device=DEV)]
+            if waits:
+                torch.cuda.synchronize()
+            c.gkv_chunk_attn(0, q, k, v, steps[0])
+            if waits:
+                torch.cuda.synchronize()
+            c.gkv_decode_attn(0, q[:, 0].contiguous(), steps[1])
+            if waits:
+                torch.cuda.synchronize()
+            kept.append(steps)
+        torch.cuda.synchronize()
+        c.gkv_bits_report(0)
+        both.append(kept)
+    for i, (a, b) in enumerate(zip(*both)):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), i
+
+
 # ---- together ----
 @pytest.mark.parametrize("turn", [5, 150])
 def test_prompt_in_pieces(turn):
