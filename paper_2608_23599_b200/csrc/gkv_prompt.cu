@@ -33,7 +33,7 @@ using attend::kPanel;
 using attend::kRows;
 using attend::kTileBytes;
 constexpr int kMaxSeqs = 1024;             // sequences of one launch
-constexpr int kFewSeqs = 32;               // the same where the parameters are to stay short
+constexpr int kFewSeqs = 32;               // the same where the parameters are short: 14 KB instead of 3 cost the host 5 us a call, of masses 2
 
 // Sequences in the order in which their work is dealt out (longest first).  Work items of sequence i: [first[i], first[i + 1]).
 template <int N>
