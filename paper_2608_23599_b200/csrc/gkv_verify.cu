@@ -5,16 +5,17 @@
 //   q . k~ = (q s) . code + q . z
 // exactly as gkv_decode.cu reads it: codes are used as they lie (a code in the mantissa of an fp16 with a zero exponent field is code 2^(p - 24)),
 // the scaled query is an fp16 pair hi + lo formed once per half block, and q . z starts the accumulators.  Values the same way with
-// the scales in the weights: O += (P s) code, and sum_j p_j z_j in four more accumulators, one per group of 32 channels.  Nothing about the logits is
-// rounded to fewer than 22 bits; weights are fp16 (2^-12 of themselves) over codes, bf16 (2^-9) over exact rows, as the bf16 output allows.
+// the scales in the weights: O += (P s) code, and sum_j p_j z_j in four more accumulators, one per group of 32 channels.  A scaled query is off by 2^-22 of
+// itself or 2^-25.  Weights are single numbers, as the bf16 output allows: bf16 (off by 2^-8 at most) over exact rows, relative to the row's reference; fp16
+// (2^-11) over codes, relative to the item's own maximum (weigh_codes, code_values), since fp16 has no room for those of a row whose keys lie far apart.
 //
 // What bounds it: at 4 bits a block of 64 tokens is 10 KB, 420 cycles of an SM's share of the copy bandwidth; its products are 212 MMAs per 16 rows,
 // 424 cycles of the SM's warp-level tensor pipes.  Tiles of 128 rows on the fifth-generation tensor cores would need the same 512 cycles for
 // any number of rows and every value written to shared memory first: with up to 64 rows a kernel of that kind took 1.9 times as long.
 //
-// What it measured: 64 streams of 32,757 tokens on mixed rungs, 20 rows, 203 us, 0.25 of the copy bandwidth: 6000 cycles for a warp's item of 106
-// MMAs and 830 other instructions, of which 25% are waits of dependent instructions on one another with three warps a scheduler, 42% issue slots used,
-// tensor pipes 30%.  More warps have no registers (68 accumulators and 16 logits each); unrolling the logits' loop by 2 and 4 took 1.06 and 1.10 times as
+// What it measured: 64 streams of 32,757 tokens on mixed rungs, 20 rows, 219 us, 0.23 of the copy bandwidth.  With weights relative to the row's
+// reference (199 us) a warp's item of 106 MMAs and 830 other instructions took 6000 cycles, of which 25% were waits of dependent instructions on one another
+// with three warps a scheduler, 42% issue slots used, tensor pipes 30%.  More warps have no registers (68 accumulators, 16 of an item and 16 logits each); unrolling the logits' loop by 2 and 4 took 1.06 and 1.10 times as
 // long (instruction cache), a rolled value loop the same.
 //
 // Work split.  gkv_chunk.h cuts the streams' items (half blocks: 32 tokens) into equal ranges, one per CTA, or every stream into the same number.  The CTA's warps form teams of
@@ -47,9 +48,9 @@ constexpr int kVMeta = 80;                 // a stage's description
 constexpr int kVPend = 64;                 // centroids that a team has collected
 constexpr int kVMaxRing = 6;
 constexpr float kVAbove = 4.f;             // log2
+constexpr float kVTop = 11.f;              // log2 of an item's heaviest weight over codes: see code_values
 constexpr int kVIdle = 1 << 22;            // fruitless looks for room after which the walk gives up
 constexpr int kVOPitch = kD + 4;           // floats of a row in the merge
-constexpr float kVUp = 1048576.f;          // 2^20: what the value accumulators lack (codes are code 2^(p - 24), weights carry 2^(4 - p))
 
 struct alignas(16) VMeta {
   uint32_t what;             // kind (0 = no more, 1 = codes, 2 = rows, 3 = centroids) | level << 8 | rows << 16
@@ -157,15 +158,14 @@ __device__ __forceinline__ void split(uint32_t q, uint32_t s, uint32_t& hi, uint
 
 struct VState {
   float o[16][4], oz[4];     // channels 8 n + 2 c4, + 1 of rows r (0, 1) and r + 8 (2, 3); groups 2 c4, + 1
-  float m0, m1, l0, l1;      // references of the two rows (units of q . k), this lane's part of their sums
+  float m0, m1, l0, l1;      // references of the two rows (log2), this lane's part of their sums
 };
 
-// x becomes the weights exp2(c (x - m)).  They stay at most 1 (a weight times a value scale of up to 4094 and 2^4 has to fit fp16); where the maximum
-// passes the reference m, m goes kVAbove beyond it, so that it does not move again for the next small step (16 rows' accumulators are rescaled for
-// it: without that in four of five steps of a team).
+// t0, t1: the largest logits of the two rows (log2).  The references stay at or above them; where a maximum passes its reference, that goes kVAbove beyond
+// it, so that it does not move again for the next small step (16 rows' accumulators are rescaled for it: without that in four of five steps of a team).
 template <int NT>
-__device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
-  float t0 = fmaxf(x[0][0], x[0][1]), t1 = fmaxf(x[0][2], x[0][3]);
+__device__ __forceinline__ void raise(VState& st, const float (&x)[NT][4], float c, float& t0, float& t1) {
+  t0 = fmaxf(x[0][0], x[0][1]), t1 = fmaxf(x[0][2], x[0][3]);
 #pragma unroll
   for (int n = 1; n < NT; ++n) {
     t0 = max3(t0, x[n][0], x[n][1]);
@@ -176,9 +176,11 @@ __device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
     t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, d));
     t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, d));
   }
+  t0 *= c;
+  t1 *= c;
   if (__any_sync(0xffffffffu, t0 > st.m0 || t1 > st.m1)) {
-    const float above = kVAbove / c, n0 = t0 > st.m0 ? t0 + above : st.m0, n1 = t1 > st.m1 ? t1 + above : st.m1;
-    const float f0 = st.m0 == -INFINITY ? 0.f : ex2((st.m0 - n0) * c), f1 = st.m1 == -INFINITY ? 0.f : ex2((st.m1 - n1) * c);
+    const float n0 = t0 > st.m0 ? t0 + kVAbove : st.m0, n1 = t1 > st.m1 ? t1 + kVAbove : st.m1;
+    const float f0 = st.m0 == -INFINITY ? 0.f : ex2(st.m0 - n0), f1 = st.m1 == -INFINITY ? 0.f : ex2(st.m1 - n1);
     st.m0 = n0;
     st.m1 = n1;
     st.l0 *= f0;
@@ -195,9 +197,14 @@ __device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
     st.oz[2] *= f1;
     st.oz[3] *= f1;
   }
-  const float a0 = st.m0 == -INFINITY ? 0.f : -st.m0 * c, a1 = st.m1 == -INFINITY ? 0.f : -st.m1 * c;
+}
+// Exact rows: x becomes the weights exp2(c x - m).  bf16 has room for any of them.
+__device__ __forceinline__ void weigh_rows(VState& st, float (&x)[2][4], float c) {
+  float t0, t1;
+  raise(st, x, c, t0, t1);
+  const float a0 = st.m0 == -INFINITY ? 0.f : -st.m0, a1 = st.m1 == -INFINITY ? 0.f : -st.m1;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+  for (int n = 0; n < 2; ++n) {
     x[n][0] = ex2(fmaf(x[n][0], c, a0));
     x[n][1] = ex2(fmaf(x[n][1], c, a0));
     x[n][2] = ex2(fmaf(x[n][2], c, a1));
@@ -205,6 +212,28 @@ __device__ __forceinline__ void weigh(VState& st, float (&x)[NT][4], float c) {
     st.l0 += x[n][0] + x[n][1];
     st.l1 += x[n][2] + x[n][3];
   }
+}
+// Codes: x becomes the weights relative to the item's own maximum, 2^kVTop for the heaviest, and g what they have to be multiplied by (in 32 bits) to be
+// exp2(c x - m).  fp16 has no room for weights relative to a row's maximum: behind a key that leads by 11 nats all others would be below 2^-16, and a weight
+// times a value scale of 2^-8 a handful of steps of 2^-24.
+__device__ __forceinline__ void weigh_codes(VState& st, float (&x)[4][4], float c, float& g0, float& g1) {
+  float t0, t1;
+  raise(st, x, c, t0, t1);
+  const float a0 = t0 == -INFINITY ? 0.f : kVTop - t0, a1 = t1 == -INFINITY ? 0.f : kVTop - t1;
+  g0 = t0 == -INFINITY ? 0.f : ex2(-a0 - st.m0);
+  g1 = t1 == -INFINITY ? 0.f : ex2(-a1 - st.m1);
+  float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    x[n][0] = ex2(fmaf(x[n][0], c, a0));
+    x[n][1] = ex2(fmaf(x[n][1], c, a0));
+    x[n][2] = ex2(fmaf(x[n][2], c, a1));
+    x[n][3] = ex2(fmaf(x[n][3], c, a1));
+    s0 += x[n][0] + x[n][1];
+    s1 += x[n][2] + x[n][3];
+  }
+  st.l0 = fmaf(s0, g0, st.l0);
+  st.l1 = fmaf(s1, g1, st.l1);
 }
 
 // Logits of a half block's 32 tokens: columns 8 n + 2 c4, + 1 of rows r, r + 8.  raw: parameters and codes of the keys; q: the rows' fragments (fp16).
@@ -245,30 +274,83 @@ __device__ __forceinline__ void code_logits(float (&x)[4][4], uint32_t raw, uint
     for (int k = 0; k < 4; ++k) x[n][k] = fmaf(x[n][k], up, z[k]);
   }
 }
-// O += P V of a half block; `raw`: where its value parameters would lie behind the keys (off_vp, off_vc).
+// The largest of a half block's value scales, as an fp16 pattern (they are not negative)
 template <int BITS>
-__device__ __forceinline__ void code_values(VState& st, const float (&x)[4][4], uint32_t raw, int lane) {
-  const int r = lane >> 2, c4 = lane & 3;
-  const __half2 up0 = __float2half2_rn(16.f), up1 = __float2half2_rn(static_cast<float>(1 << (4 - code_exp(BITS, 1))));
+__device__ __forceinline__ uint32_t largest_scale(uint32_t raw, int lane) {
+  uint32_t top = 0;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const uint32_t a[4] = {f16_pair(x[2 * t][0], x[2 * t][1]), f16_pair(x[2 * t][2], x[2 * t][3]), f16_pair(x[2 * t + 1][0], x[2 * t + 1][1]),
-                           f16_pair(x[2 * t + 1][2], x[2 * t + 1][3])};
-    const uint32_t vp = raw + off_vp(BITS, t);
-    uint2 z = lds64(vp + 128 + ((r & 3) * 4 + c4) * 8);      // column r: group r
-    if (r >= 4) z.x = z.y = 0u;
-    mma_f16(st.oz, a, z.x, z.y);
+    const uint32_t at = raw + off_vp(BITS, t) + (lane & 3) * 32;
+    const uint4 x = lds128(at), y = lds128(at + 16);
+    top = __vmaxu2(top, __vmaxu2(__vmaxu2(__vmaxu2(x.x, x.y), __vmaxu2(x.z, x.w)), __vmaxu2(__vmaxu2(y.x, y.y), __vmaxu2(y.z, y.w))));
+  }
+  return __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+}
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+// O += P V of a half block; `raw`: where its value parameters would lie behind the keys (off_vp, off_vc); g: see weigh_codes.
+// The products P s are single fp16 numbers, in the middle of their range whatever the values' size: with the largest scale below 2^-b the
+// scales are multiplied by 2^b (exactly; where b < 0, the weights are), and the item's sum leaves by one multiplication in 32 bits.  So
+// a product is off by 2^-11 of itself or by 2^-36 of the item's heaviest key's.  Items without that, weights relative to the row's reference and
+// scales times 16: 199 us for 64 streams of 32,757 tokens, 20 rows, but outputs off by tenths of their norm behind a leading key.
+template <int BITS>
+__device__ __forceinline__ void code_values(VState& st, const float (&x)[4][4], uint32_t raw, int lane, float g0, float g1) {
+  const int r = lane >> 2, c4 = lane & 3;
+  const uint32_t top = largest_scale<BITS>(raw, lane);
+  const int b = min(11, 14 - static_cast<int>(top >> 10)), up = max(b, 0) + 4;
+  // 2^up and, for the tokens whose codes lie higher, 2^(up - p)
+  const __half2 up0 = h2(static_cast<uint32_t>(up + 15) * 0x04000400u), up1 = h2(static_cast<uint32_t>(up + 15 - code_exp(BITS, 1)) * 0x04000400u);
+  uint32_t a[2][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint2 s = lds64(vp + c4 * 32 + j * 8);
+  for (int t = 0; t < 2; ++t) {
+    a[t][0] = f16_pair(x[2 * t][0], x[2 * t][1]);
+    a[t][1] = f16_pair(x[2 * t][2], x[2 * t][3]);
+    a[t][2] = f16_pair(x[2 * t + 1][0], x[2 * t + 1][1]);
+    a[t][3] = f16_pair(x[2 * t + 1][2], x[2 * t + 1][3]);
+  }
+  float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    uint2 z = lds64(raw + off_vp(BITS, t) + 128 + ((r & 3) * 4 + c4) * 8);      // column r: group r
+    if (r >= 4) z.x = z.y = 0u;
+    mma_f16(zero, a[t], z.x, z.y);
+  }
+  st.oz[0] = fmaf(zero[0], g0, st.oz[0]);
+  st.oz[1] = fmaf(zero[1], g0, st.oz[1]);
+  st.oz[2] = fmaf(zero[2], g1, st.oz[2]);
+  st.oz[3] = fmaf(zero[3], g1, st.oz[3]);
+  if (b < 0) {
+    const float down = exp2i(b);
+    const __half2 d = __float2half2_rn(down);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[t][k] = u32(__hmul2(h2(a[t][k]), d));
+  }
+  const float out = exp2i(20 - b);             // codes are code 2^(p - 24)
+  const uint64_t f0 = f2_pack(g0 * out, g0 * out), f1 = f2_pack(g1 * out, g1 * out);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float o[4][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint2 s = lds64(raw + off_vp(BITS, t) + c4 * 32 + j * 8);
       const __half2 s0 = __hmul2(h2(s.x), up0), s1 = __hmul2(h2(s.y), up1);
-      const uint32_t ps[4] = {u32(__hmul2(h2(a[0]), s0)), u32(__hmul2(h2(a[1]), s0)), u32(__hmul2(h2(a[2]), s1)), u32(__hmul2(h2(a[3]), s1))};
+      const uint32_t ps[4] = {u32(__hmul2(h2(a[t][0]), s0)), u32(__hmul2(h2(a[t][1]), s0)), u32(__hmul2(h2(a[t][2]), s1)), u32(__hmul2(h2(a[t][3]), s1))};
       uint32_t w[4];
       lane_words<BITS>(raw + off_vc(BITS, t), j, lane, w);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) mma_f16(st.o[4 * j + 2 * i + k], ps, code_bits<BITS, true>(w, i, k), code_bits<BITS, true>(w, i, k + 2));
+        for (int k = 0; k < 2; ++k) mma_f16(o[2 * i + k], ps, code_bits<BITS, true>(w, i, k), code_bits<BITS, true>(w, i, k + 2));
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      float (&to)[4] = st.o[4 * j + n];
+      f2_unpack(f2_fma(f2_pack(o[n][0], o[n][1]), f0, f2_pack(to[0], to[1])), to[0], to[1]);
+      f2_unpack(f2_fma(f2_pack(o[n][2], o[n][3]), f1, f2_pack(to[2], to[3])), to[2], to[3]);
     }
   }
 }
@@ -605,15 +687,16 @@ __global__ void __launch_bounds__(kVThreads, 1)
               for (int k = 0; k < 4; ++k)
                 if (hide >> (8 * n + 2 * c4 + (k & 1)) & 1u) x[n][k] = -INFINITY;
           }
-          weigh<4>(st, x, c);
+          float g0, g1;
+          weigh_codes(st, x, c, g0, g1);
           if (level == 8) {
             free_part();
             if (!(ok = wait_part())) break;
-            code_values<8>(st, x, ring + got_at * kVStage - half_bytes(8) / 2, lane);
+            code_values<8>(st, x, ring + got_at * kVStage - half_bytes(8) / 2, lane, g0, g1);
           } else if (level == 4) {
-            code_values<4>(st, x, raw, lane);
+            code_values<4>(st, x, raw, lane, g0, g1);
           } else {
-            code_values<2>(st, x, raw, lane);
+            code_values<2>(st, x, raw, lane, g0, g1);
           }
           free_part();
         } else {
@@ -657,12 +740,10 @@ __global__ void __launch_bounds__(kVThreads, 1)
                 if (j >= n || (hide >> j & 1u) || (causal >= 0 && causal + j > (k < 2 ? tok_a : tok_b))) x[t][k] = -INFINITY;
               }
           }
-          weigh<2>(st, x, c);
+          weigh_rows(st, x, c);
           free_part();
           if (!(ok = wait_part())) break;
-          const float down = 1.f / kVUp;
-          const uint32_t a[4] = {bf16_pair(x[0][0] * down, x[0][1] * down), bf16_pair(x[0][2] * down, x[0][3] * down), bf16_pair(x[1][0] * down, x[1][1] * down),
-                                 bf16_pair(x[1][2] * down, x[1][3] * down)};
+          const uint32_t a[4] = {bf16_pair(x[0][0], x[0][1]), bf16_pair(x[0][2], x[0][3]), bf16_pair(x[1][0], x[1][1]), bf16_pair(x[1][2], x[1][3])};
           const uint32_t vraw = ring + got_at * kVStage;
           if (swizzled && n < 16) {          // rows that are not there may hold anything: zeros (every warp of the team writes the same ones)
             for (int i = n * 8 + lane; i < 128; i += 32) {
@@ -696,10 +777,10 @@ __global__ void __launch_bounds__(kVThreads, 1)
         const float z0 = __shfl_sync(0xffffffffu, st.oz[g & 1], from), z1 = __shfl_sync(0xffffffffu, st.oz[2 + (g & 1)], from);
 #pragma unroll
         for (int n = 4 * g; n < 4 * g + 4; ++n) {
-          st.o[n][0] = fmaf(st.o[n][0], kVUp, z0);
-          st.o[n][1] = fmaf(st.o[n][1], kVUp, z0);
-          st.o[n][2] = fmaf(st.o[n][2], kVUp, z1);
-          st.o[n][3] = fmaf(st.o[n][3], kVUp, z1);
+          st.o[n][0] += z0;
+          st.o[n][1] += z0;
+          st.o[n][2] += z1;
+          st.o[n][3] += z1;
         }
       }
     }
@@ -715,8 +796,8 @@ __global__ void __launch_bounds__(kVThreads, 1)
         *reinterpret_cast<float2*>(d0 + 8 * kVOPitch + 8 * n) = make_float2(st.o[n][2], st.o[n][3]);
       }
       if (c4 == 0) {
-        mml[warp * 16 + r] = make_float2(st.m0 * c, st.l0);
-        mml[warp * 16 + r + 8] = make_float2(st.m1 * c, st.l1);
+        mml[warp * 16 + r] = make_float2(st.m0, st.l0);
+        mml[warp * 16 + r + 8] = make_float2(st.m1, st.l1);
       }
     }
     fence_async();                         // (copies land there next)
