@@ -4,7 +4,7 @@
 // A CTA works on tiles of 256 rows in two halves; the rows of a half are the g query heads of 128 / g consecutive tokens, so that all of them read one KV
 // head and the diagonal is 128 / g tokens wide.  Per step of 128 keys and half:
 //   S = Q K^T            both operands in shared memory, fp32 accumulator in tensor memory (where keys are pairs, + Q K_lo^T)
-//   m' = max(m, row max) the reference m moves only when the maximum has grown by more than 2^8: P then stays below 2^8, and the
+//   m' = max(m, row max) the reference m moves only when the maximum has grown by more than 2^8: P then stays below 2^8 (2^15 as fp16: kUp), and the
 //                        accumulator is rescaled a handful of times per row, not once per step
 //   P = exp2(c S - c m)  16 bits, over S in tensor memory; its sum l is taken before it is rounded
 //   O += P V             P from tensor memory, V as it lies ([token][channel], MN-major); it starts on three quarters of P
@@ -47,6 +47,10 @@ constexpr int kLaunchRegs = 168, kSoftRegs = 216, kOtherRegs = 72;
 static_assert(2 * kSoftRegs + kOtherRegs <= 3 * kLaunchRegs, "a split draws on the launch's registers");
 constexpr int kStart = 2, kSnap = 1;        // steps that a part's beginning and end cost (chunk_plan); how near to a tile's end a cut is not worth slots
 constexpr float kSlack = 8.f;              // log2 of what a weight may exceed 1 by before the reference moves
+// log2 of what all weights are multiplied by.  As fp16 they then reach from 2^15 (a row's maximum kSlack above its reference) down to 2^-14 with all their
+// bits: 2^-21 of the reference's, where 2^-14 was off by a hundredth of the norm behind a key that leads the others by 14.5 nats.
+template <class Work>
+constexpr float kUp = Work::kBf16 ? 0.f : 7.f;
 constexpr int kEarly = 6;                  // k-steps of P V that start early, of eight
 
 // A CTA's part of a tile, as `Work::next` describes it.
@@ -234,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
           }
         }
         if (move) m = top;
-        const float at = m == -INFINITY ? 0.f : -m * c;
+        const float at = m == -INFINITY ? 0.f : fmaf(-m, c, kUp<Work>);
         const uint64_t cc = f2_pack(c, c), mm = f2_pack(at, at);
         uint64_t sum0 = 0, sum1 = 0;
 #pragma unroll
@@ -315,8 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
         }
       }
       if (real) {
-        if (to >= 0) work.part_ml[static_cast<size_t>(to) * 2 * kRows + slot_row] = make_float2(m * c, ok ? l : NAN);
-        else if (work.lse) work.lse[row * work.n_q_heads + hq] = ok ? lse_of(work, m * c, l) : NAN;
+        if (to >= 0) work.part_ml[static_cast<size_t>(to) * 2 * kRows + slot_row] = make_float2(fmaf(m, c, -kUp<Work>), ok ? l : NAN);
+        else if (work.lse) work.lse[row * work.n_q_heads + hq] = ok ? lse_of(work, fmaf(m, c, -kUp<Work>), l) : NAN;
       }
       tmem_before();
     }

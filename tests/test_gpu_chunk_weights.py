@@ -138,3 +138,12 @@ def test_large_and_small_values(level, gain):
     c, oc = streams_alike(k, v, plan(ctx, level), 20, 8, 4)
     if not beyond_the_format(c, v[64:], level):
         run_alike(c, oc, *x, 20, 8)
+
+
+@pytest.mark.parametrize("level", [16, 8, 4, 2])
+@pytest.mark.parametrize("lead,noise", [(11.0, 0.3), (13.0, 0.0), (14.5, 0.0)])
+def test_a_leading_key_and_many_rows(level, lead, noise):
+    ctx = 64 * 130 + 5
+    k, v, x = sink(ctx, 40, 4, lead, 1.0, noise, seed=level)
+    c, oc = streams_alike(k, v, plan(ctx, level), 1, 2, 4)
+    run_alike(c, oc, *x, 1, 2)
