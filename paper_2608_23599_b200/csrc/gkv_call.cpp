@@ -282,6 +282,7 @@ PyObject* py_prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return refuse();
   size_t need = 0, have = 0;
   void* ws = nullptr;
+  PyObject* held = nullptr;                // the workspace's owner: while the launches are made another thread may put a new one into its place
   int rc = f_prompt_bytes(&d, &need);
   if (rc == GKV_OK && need > 0) {
     PyObject* space = a[7];
@@ -298,12 +299,15 @@ PyObject* py_prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (space && PyTuple_Check(space) && PyTuple_GET_SIZE(space) >= 2 && as_plain(PyTuple_GET_ITEM(space, 0), &ws)) have = PyLong_AsSize_t(PyTuple_GET_ITEM(space, 1));
     if (PyErr_Occurred()) return refuse();
     if (have < need) return PyLong_FromSize_t(need);
+    held = space;
+    Py_INCREF(held);
   }
   if (rc == GKV_OK) {
     Py_BEGIN_ALLOW_THREADS
     rc = f_prompt_attn(&d, q.ptr, k.ptr, v.ptr, out.ptr, static_cast<float*>(lse.ptr), ws, have, st);
     Py_END_ALLOW_THREADS
   }
+  Py_XDECREF(held);
   return PyLong_FromLong(rc);
 }
 
