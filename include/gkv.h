@@ -189,7 +189,8 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
  *          8 bits or more, values with 11; keys and logits keep 22
  *   lse    device fp32 [batch][n_new][n_q_heads], natural-log sum of exp(logit), or NULL
  *   workspace  device, 16-byte aligned, gkv_chunk_workspace_bytes long: partial results of the call, free again when its kernels
- *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too)
+ *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too); the launches of calls of
+ *          several host threads with one workspace on one stream are not mixed
  * All buffers and the arena must lie on the current device (GKV_ERR_INVALID_ARG else).  The bits that the call reads are not counted by gkv_bits_report.
  * A captured call replays the context length of its capture: capture again after an append. */
 GKV_API int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len,
@@ -225,7 +226,8 @@ typedef struct gkv_prompt {
  *   lse  device fp32 [rows][n_q_heads], packed, natural-log sum of exp(logit), or NULL
  *   workspace  device, 16-byte aligned, or NULL.  With gkv_prompt_workspace_bytes of it (0 for many shapes, below 40 MB for all) work whose
  *        longest part would hold up the rest is cut into equal ranges; with less the result is the same to rounding, later.  Calls that may
- *        run at the same time need workspaces of their own (two captured graphs too) */
+ *        run at the same time need workspaces of their own (two captured graphs too); the launches of calls of several host threads with one
+ *        workspace on one stream are not mixed */
 GKV_API int gkv_prompt_attn(const gkv_prompt* p, const void* q, const void* k, const void* v, void* out, float* lse, void* workspace, size_t workspace_bytes,
                             void* stream);
 GKV_API int gkv_prompt_workspace_bytes(const gkv_prompt* p, size_t* bytes);      /* bytes: host out */

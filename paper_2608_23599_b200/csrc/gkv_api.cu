@@ -2092,12 +2092,14 @@ int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new
     ChunkMerge merge;
     if (!workspace || workspace_bytes < verify_bytes(c)) return GKV_ERR_INVALID_ARG;      // (whatever this call's cuts need)
     chunk_plan(call.shape, len, verify_min_items(call.shape), 0, 0, verify_second(call.shape), &cuts, &merge);
+    std::lock_guard<std::mutex> lock(launching(workspace));
     CK(c, launch_verify(call, cuts, merge, len, st));
     return GKV_OK;
   }
   dense_shape(&call.shape, dense_rows(c, L));
   const int seqs = workspace ? dense_group(call.shape, L.n_closed, workspace_bytes) : 0;
   if (seqs == 0) return GKV_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lock(launching(workspace));
   for (int b = 0; b < c->cfg.batch; b += seqs) CK(c, launch_dense(call, b, std::min(seqs, c->cfg.batch - b), len, st));
   return GKV_OK;
 }

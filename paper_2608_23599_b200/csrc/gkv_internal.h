@@ -6,6 +6,7 @@
 
 #include <atomic>
 #include <initializer_list>
+#include <mutex>
 
 #include "gkv_layout.cuh"
 
@@ -202,6 +203,13 @@ cudaError_t raise_smem_limit(void (*kernel)(Args...), size_t bytes, std::atomic<
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
+}
+
+// Held while a call makes the launches that hand results on in `workspace`.  Host threads that call on one stream with its workspace (torch's default stream
+// is every thread's) find their calls behind one another on the device, not their launches mixed.  Few addresses share a mutex.
+inline std::mutex& launching(const void* workspace) {
+  static std::mutex all[64];
+  return all[(reinterpret_cast<uintptr_t>(workspace) >> 9) * 0x9e3779b97f4a7c15ull >> 58];
 }
 
 // Whether all are memory of the current device, or memory that every device reaches (null pointers aside): the tensor-map kernels must not be given

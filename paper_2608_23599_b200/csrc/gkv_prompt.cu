@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -544,6 +545,8 @@ int attn(const gkv_prompt* d, const void* q, const void* k, const void* v, void*
     w.ln2_rest = static_cast<float>(logit_of(d) - kLn2);
     return launch_prompt(w, d, order, at, end, maps, workspace, workspace_bytes, st);
   };
+  std::unique_lock<std::mutex> lock;
+  if (workspace) lock = std::unique_lock<std::mutex>(launching(workspace));
   const int n = static_cast<int>(order.size());
   for (int at = 0; at < n; at += kMaxSeqs) {
     const int end = std::min(n, at + kMaxSeqs);
