@@ -42,7 +42,7 @@ constexpr int kTileBytes = 2 * kPanel;
 constexpr int kThreads = 384;              // softmax of the halves (four warps each), loads, products, value rows behind a sequence, parts
 constexpr int kStages = 5;
 constexpr int kOffStage = 2 * kTileBytes, kOffBar = kOffStage + kStages * kTileBytes;
-constexpr int kParts = 3, kOffParts = kOffBar + 336, kSmem = kOffParts + kParts * 64 + 1024;
+constexpr int kParts = 3, kOffParts = kOffBar + 336, kOffLeft = kOffParts + kParts * 64, kSmem = kOffLeft + 80 + 1024;
 constexpr int kLaunchRegs = 168, kSoftRegs = 216, kOtherRegs = 72;
 static_assert(2 * kSoftRegs + kOtherRegs <= 3 * kLaunchRegs, "a split draws on the launch's registers");
 constexpr int kStart = 2, kSnap = 1;        // steps that a part's beginning and end cost (chunk_plan); how near to a tile's end a cut is not worth slots
@@ -64,6 +64,12 @@ struct alignas(16) Part {
   uint8_t keep;                            // value rows of the last step that count, 128 = all
 };
 static_assert(sizeof(Part) == 64, "");
+// What the warp that works out the parts leaves: how many it published, and after a given-up wait the part that it had in hand, with the walk's state.
+struct Left {
+  Part part;
+  int published, hand, state, slot;
+};
+static_assert(sizeof(Left) == 80 && kSmem <= 227 * 1024, "");
 struct Maps {
   CUtensorMap q, k, k_lo, v;
 };
@@ -77,13 +83,41 @@ struct Maps {
 //   load_keys(map, dst, part, step, bar) a step's 128 rows (two panels)
 //   flags(part, step), term(part, step)  kPairs only
 //   place(tile)                          where a tile lies (tok0, len, row0, head0)
-//   fail()                               a wait was given up
+//   fail()                               a wait was given up (the rows of the CTA's parts that are not done are NaN)
 constexpr int kHasTerm = 1, kHasLow = 2;
 
 // The log-sum-exp of weights 2^(x - top) that sum to `sum`; ln2_rest: what a logit is more of itself than its 32 bits say
 template <class Work>
 __device__ __forceinline__ float lse_of(const Work& work, float top, float sum) {
   return fmaf(top, kLn2, fmaf(top, work.ln2_rest, lg2(sum) * kLn2));
+}
+
+// NaN for the rows of a part, or into its slot, from which the merge takes it on
+template <class Work>
+__device__ __forceinline__ void spoil(const Work& work, const Part& x) {
+  for (int i = threadIdx.x; i < 2 * work.half_tokens * work.group; i += kThreads) {
+    const int tok = x.tok0 + i / work.group;
+    if (tok >= x.len) continue;
+    if (x.slot >= 0) {
+      work.part_ml[static_cast<size_t>(x.slot) * 2 * kRows + i] = make_float2(NAN, NAN);
+      continue;
+    }
+    const int64_t row = x.row0 + tok;
+    const int head = x.head0 + i % work.group;
+    uint4* const to = reinterpret_cast<uint4*>(work.out + row * work.out_stride + head * kD);
+#pragma unroll 1
+    for (int k = 0; k < kD / 8; ++k) to[k] = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+    if (work.lse) work.lse[row * work.n_q_heads + head] = NAN;
+  }
+}
+// (a function of its own: inside the kernel it cost others their registers, 84 -> 85.5 us of a batch of prompts)
+template <class Work>
+__device__ __noinline__ void spoil_left(const Work& work, const Part* ring, const Left* left) {
+  int state = left->state, slot = left->slot;
+  parts_left<kParts>(
+      ring, left->published, left->hand != 0, left->part, [&](Part& x) { return !work.whole_tiles() && work.next(state, slot, x); },
+      [&](const Part& x) { spoil(work, x); });
+  if (threadIdx.x == 0) work.fail();
 }
 
 template <class Work>
@@ -100,6 +134,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(base + kOffBar + 308);
   static_assert(120 + 16 * kStages + 16 * kParts <= 304, "room for the barriers");
   Part* const ring = reinterpret_cast<Part*>(base + kOffParts);
+  Left* const left = reinterpret_cast<Left*>(base + kOffLeft);
 
   if (threadIdx.x == 0) {
     bar_init(bar_q, 1);
@@ -324,7 +359,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       }
       tmem_before();
     }
-    if (!ok && lane == 0) work.fail();
   } else {
     fewer_regs<kOtherRegs>();
     if (warp == 8) {
@@ -462,7 +496,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
       // Whole tiles: the CTA's own, then those of CTAs that have not been launched yet and are called off here (heaviest first, as they come)
       const bool whole = work.whole_tiles();
       uint32_t tile = blockIdx.x;
-      for (int n = 0;; ++n) {
+      bool hand = false;
+      int n = 0;
+      for (;; ++n) {
         if (n > 0 && whole) {
           // not before the last step of the tile before is being loaded: a tile called off early is one that no idle CTA can have
           if (!bar_wait(bar_more, (n - 1) & 1, abort)) break;
@@ -471,6 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
           call_off(answer, bar_call);
           if (!bar_wait(bar_call, (n - 1) & 1, abort)) {
             bar_drain(bar_call, (n - 1) & 1);
+            hand = bar_poll(bar_call, (n - 1) & 1) && called_off(answer, tile);
+            if (hand) work.whole(tile, x);
             break;
           }
           more = called_off(answer, tile);
@@ -479,10 +517,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
           more = work.next(state, slot, x);
         }
         if (!more) x.tile = -1;
+        hand = more;
         if (n >= kParts && !bar_wait(bar_got + 8 * (n % kParts), (n / kParts - 1) & 1, abort)) break;
         ring[n % kParts] = x;
         bar_arrive(bar_put + 8 * (n % kParts));
-        if (!more) break;
+        hand = false;
+        if (!more) {
+          ++n;
+          break;
+        }
+      }
+      left->published = n;
+      left->hand = hand;
+      if (hand) {
+        left->part = x;
+        left->state = state;
+        left->slot = slot;
       }
     }
   }
@@ -490,6 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const __grid_consta
   tmem_before();
   __syncthreads();
   if (warp == 9) tmem_dealloc(tmem, 512);
+  if (*abort) spoil_left(work, ring, left);      // (whoever was inside a part has written NaN itself)
 }
 
 // Merges the slots of tiles that were cut, in their order: 32 rows of a tile per CTA, a lane per row, 32 channels per warp.

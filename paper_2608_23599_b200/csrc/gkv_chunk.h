@@ -99,6 +99,21 @@ inline int cut_tiles(int tiles, int64_t total, int n_ctas, int start, int snap, 
   return slots;
 }
 
+// After a given-up wait: f(part) for every part of a CTA that some of its warps may not have begun (and perhaps for some that they have done).  A part is put
+// over the one kRing before it once all warps have begun that one, so what they have not begun is in the ring (`published` went through it, one without a
+// tile at the end), in hand (`hand`: `part` was taken, but not published), or still to come (next(part), with a part in hand only).
+template <int kRing, class Part, class Next, class F>
+#if defined(__CUDACC__)
+__host__ __device__
+#endif
+inline void parts_left(const Part* ring, int published, bool hand, Part part, Next next, F f) {
+  for (int k = published > kRing ? published - kRing : 0; k < published; ++k)
+    if (ring[k % kRing].tile >= 0) f(ring[k % kRing]);
+  if (!hand) return;
+  do f(part);
+  while (next(part));
+}
+
 // CTAs for so much work, where one is worth starting for min_items
 inline int chunk_ctas(int64_t total, int min_items) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kChunkCtas, total / min_items))); }
 

@@ -130,7 +130,7 @@ struct PromptWork {
     const auto at = tiles.place(tile);
     return {at.tok0, at.len, at.head * group, tiles.seqs.row[at.seq]};
   }
-  __device__ __forceinline__ void fail() const {}      // (the rows without a result are NaN)
+  __device__ __forceinline__ void fail() const {}      // (a prompt has no status word: its NaN rows say it)
 };
 
 // ---- masses of prompt tokens ---------------------------------------------------------------------
