@@ -214,7 +214,7 @@ typedef struct gkv_prompt {
   const int32_t* offsets; /* HOST int32 [n_seqs + 1], ascending from >= 0; read during the call only */
   int64_t q_stride, k_stride, v_stride, out_stride; /* elements from one row to the next, a multiple of 8; 0 = heads * head_dim.
                                                        (A row's heads follow one another: rows may be slices of a fused projection.) */
-  float softmax_scale;    /* 0 -> 1/sqrt(head_dim) */
+  float softmax_scale;    /* 0 -> 1/sqrt(head_dim); else positive, finite and not subnormal (GKV_ERR_INVALID_ARG) */
 } gkv_prompt;
 
 /* Causal attention of every query head over the exact rows of its own sequence (Sec. 3.1, Eq. 1 before anything is demoted):

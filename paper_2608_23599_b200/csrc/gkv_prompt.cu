@@ -357,6 +357,7 @@ int check_prompt(const gkv_prompt* d, int* rows) {
   if (!d || d->struct_size != sizeof(gkv_prompt) || d->abi_version != GKV_ABI_VERSION) return GKV_ERR_INVALID_ARG;
   if (d->n_seqs < 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->n_q_heads % d->n_kv_heads != 0) return GKV_ERR_INVALID_ARG;
   if (d->head_dim != kD || d->n_q_heads / d->n_kv_heads > kMaxHeadsPerKv) return GKV_ERR_UNSUPPORTED;
+  if (d->softmax_scale != 0.f && !(std::isnormal(d->softmax_scale) && d->softmax_scale > 0.f)) return GKV_ERR_INVALID_ARG;
   if (!d->offsets || d->offsets[0] < 0) return GKV_ERR_INVALID_ARG;
   for (int i = 0; i < d->n_seqs; ++i)
     if (d->offsets[i + 1] < d->offsets[i]) return GKV_ERR_INVALID_ARG;
