@@ -191,7 +191,7 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
  *   workspace  device, 16-byte aligned, gkv_chunk_workspace_bytes long: partial results of the call, free again when its kernels
  *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too); the launches of calls of
  *          several host threads with one workspace on one stream are not mixed
- * All buffers and the arena must lie on the current device (GKV_ERR_INVALID_ARG else).  The bits that the call reads are not counted by gkv_bits_report.
+ * n_new: 1 .. 2^30 (GKV_ERR_INVALID_ARG else).  All buffers and the arena must lie on the current device (GKV_ERR_INVALID_ARG else).  The bits that the call reads are not counted by gkv_bits_report.
  * A captured call replays the context length of its capture: capture again after an append. */
 GKV_API int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len,
                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -2037,7 +2037,7 @@ int dense_group(const ChunkShape& s, int n_closed, size_t bytes) {
 }  // namespace
 
 int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t* bytes) {
-  if (!c || !bytes || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0) return GKV_ERR_INVALID_ARG;
+  if (!c || !bytes || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0 || n_new > kChunkMaxNew) return GKV_ERR_INVALID_ARG;
   if (is_mla(c->cfg)) return GKV_ERR_UNSUPPORTED;
   const LayerState& L = c->layers[layer];
   ChunkShape s = chunk_of(c, n_new);
@@ -2053,7 +2053,7 @@ int gkv_chunk_workspace_bytes(gkv_cache* c, int32_t layer, int32_t n_new, size_t
 
 int gkv_chunk_attn(gkv_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new, int32_t n_new, const int32_t* len, void* out,
                    float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!c || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0) return GKV_ERR_INVALID_ARG;
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || n_new <= 0 || n_new > kChunkMaxNew) return GKV_ERR_INVALID_ARG;
   if (is_mla(c->cfg)) return GKV_ERR_UNSUPPORTED;
   if (!q || !k_new || !v_new || !out) return GKV_ERR_INVALID_ARG;
   if (misaligned(q, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(out, 16) || misaligned(lse, 4) || misaligned(workspace, 16))

@@ -18,6 +18,7 @@ constexpr int kChunkParts = 2 * kChunkCtas;      // most slots of a call (a CTA 
 constexpr int kChunkSlotFloats = kChunkRows * (128 + 2);
 
 constexpr int kChunkMaxBatch = 1024;       // sequences of a call with lengths of their own
+constexpr int kChunkMaxNew = 1 << 30;      // new tokens of a sequence (far more than any memory holds): what is counted of them fits 32 bits
 
 struct ChunkShape {
   int32_t batch, n_kv_heads, group, n_new;
