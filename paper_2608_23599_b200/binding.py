@@ -299,6 +299,9 @@ def _prompt_space(device, need):
         captured = torch._C._cuda_isCurrentStreamCapturing()
         kept = None if captured else _prompt_spaces.get(key)
         if kept is None or kept[1] < need:
+            kept = None
+            if not captured:                 # (the small one goes before the large one comes)
+                _prompt_spaces.pop(key, None)
             t = torch.empty(need, dtype=torch.uint8, device=device)
             kept = t.data_ptr(), need, t
             if not captured:
@@ -483,6 +486,9 @@ class Cache:
             capturing = False
         kept = None if capturing else self._chunk_spaces.get(st)
         if kept is None or kept[0][1] < need:
+            kept = None
+            if not capturing:                # (the small one goes before the large one comes)
+                self._chunk_spaces.pop(st, None)
             with torch.cuda.device(dev):
                 if handle is None:
                     t = torch.empty(need, dtype=torch.uint8, device=dev)
