@@ -13,7 +13,7 @@
 // 424 cycles of the SM's warp-level tensor pipes.  Tiles of 128 rows on the fifth-generation tensor cores would need the same 512 cycles for
 // any number of rows and every value written to shared memory first: with up to 64 rows a kernel of that kind took 1.9 times as long.
 //
-// What it measured: 64 streams of 32,757 tokens on mixed rungs, 20 rows, 219 us, 0.23 of the copy bandwidth.  With weights relative to the row's
+// What it measured: 64 streams of 32,757 tokens on mixed rungs, 20 rows, 220 us, 0.23 of the copy bandwidth.  With weights relative to the row's
 // reference (199 us) a warp's item of 106 MMAs and 830 other instructions took 6000 cycles, of which 25% were waits of dependent instructions on one another
 // with three warps a scheduler, 42% issue slots used, tensor pipes 30%.  More warps have no registers (68 accumulators, 16 of an item and 16 logits each); unrolling the logits' loop by 2 and 4 took 1.06 and 1.10 times as
 // long (instruction cache), a rolled value loop the same.
@@ -137,12 +137,21 @@ __device__ __forceinline__ uint32_t code_bits(const uint32_t (&w)[4], int i, int
   if constexpr (BITS == 8) {
     return __byte_perm(w[2 * i + (a >> 1)], 0u, a & 1 ? 0x4341 : 0x4240);
   } else if constexpr (BITS == 4) {
-    return (x ? w[i] >> 8 : w[i]) & (y ? 0x00f000f0u : 0x000f000fu);
-  } else {
+    if constexpr (V) return (x ? w[i] >> 8 : w[i]) & (y ? 0x00f000f0u : 0x000f000fu);
+    else return (x ? w[i] >> 6 : w[i] << 2) & (y ? 0x03c003c0u : 0x003c003cu);
+  } else if constexpr (V) {
     return (w[0] >> (4 * i + 8 * x)) & (y ? 0x000c000cu : 0x00030003u);
+  } else {
+    const int up = 6 - 4 * i - 8 * x;
+    return (up > 0 ? w[0] << up : w[0] >> -up) & (y ? 0x03000300u : 0x00c000c0u);
   }
 }
-__device__ __forceinline__ constexpr int code_exp(int bits, int y) { return y == 0 || bits == 8 ? 0 : bits == 4 ? 4 : 2; }
+// Keys' codes are moved up in the mantissa (to bits 6 and 8, or 2 and 6): a product with a number that begins with n zeros is added with n bits fewer.  Two bits
+// at 0 and 2 left 15 of a logit's bits (off by 1.4e-3 at 60), four at 0 and 4 left 17.
+template <bool V>
+__device__ __forceinline__ constexpr int code_exp(int bits, int y) {
+  return bits == 8 ? 0 : bits == 4 ? 4 * y + (V ? 0 : 2) : 2 * y + (V ? 0 : 6);
+}
 
 // q s as an fp16 pair: the rounded product and what is left of it (exact)
 __device__ __forceinline__ void split(uint32_t q, uint32_t s, uint32_t& hi, uint32_t& lo) {
@@ -269,7 +278,7 @@ __device__ __forceinline__ void code_logits(float (&x)[4][4], uint32_t raw, uint
   }
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
-    const float up = static_cast<float>(1 << (24 - code_exp(BITS, n & 1)));
+    const float up = static_cast<float>(1 << (24 - code_exp<false>(BITS, n & 1)));
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[n][k] = fmaf(x[n][k], up, z[k]);
   }
@@ -299,7 +308,7 @@ __device__ __forceinline__ void code_values(VState& st, const float (&x)[4][4], 
   const uint32_t top = largest_scale<BITS>(raw, lane);
   const int b = min(11, 14 - static_cast<int>(top >> 10)), up = max(b, 0) + 4;
   // 2^up and, for the tokens whose codes lie higher, 2^(up - p)
-  const __half2 up0 = h2(static_cast<uint32_t>(up + 15) * 0x04000400u), up1 = h2(static_cast<uint32_t>(up + 15 - code_exp(BITS, 1)) * 0x04000400u);
+  const __half2 up0 = h2(static_cast<uint32_t>(up + 15) * 0x04000400u), up1 = h2(static_cast<uint32_t>(up + 15 - code_exp<true>(BITS, 1)) * 0x04000400u);
   uint32_t a[2][4];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {

@@ -1,6 +1,13 @@
 """Chunks whose weights lie far apart: one key that leads all others (an attention sink, as a rule the context's first token), logits that rise along
 the context, values of any size.  A light key's weight and its value's codes have to come through as well as a heavy one's.  Bounds: those of the chunk
-operator's own tests, relative to what the keys contribute; the leading key's value is zero, so that the others are all of the output."""
+operator's own tests (logits, log-sum-exps, weights, values, output), relative to what the keys contribute; in most tests the leading key's value is
+zero, so that the others are all of the output.  Weights are fp16 numbers over codes and where there are many rows, so that there is an end to that:
+a number below 2^-14 is off by up to 2^-25.
+  Few rows: 2^11 is the heaviest weight of an item of 32 keys, at most the row's heaviest.  A weight is off by 2^-36 of that, and what it multiplies
+  (scale * code and the zero point) is at most three times the token's largest value.  The products of weights and scales have 2^14 at least where
+  the item's heaviest weight and largest scale meet: off by 2^-39 of it, times a code, less than a quarter of the former for 8 bits and less.
+  Many rows: 2^7 is the weight at the reference, which the row's heaviest reaches.  A weight is off by 2^-32 of that.
+With 1.25 * 3 * 2^-36 * max_c |v_jc| and 2^-32 |v_jc| summed over the keys the output is off by that much more, in 32-bit terms nothing."""
 import math
 
 import numpy as np
@@ -9,7 +16,7 @@ import torch
 
 from oracle import gkv_oracle as O
 from paper_2608_23599_b200 import binding as B
-from tests.test_gpu_chunk import check, f32
+from tests.test_gpu_chunk import f32
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -25,6 +32,35 @@ def streams_alike(k, v, levels, batch, n_kv, group):
     spread = [x.to(DEV)[None, :, None].expand(batch, ctx, n_kv, 128).contiguous() for x in (k, v)]
     c.gkv_append_demote(0, *spread, level_plan=np.broadcast_to(levels, (batch, n_kv, len(levels))).copy())
     return c, oc
+
+
+def check(out, lse, oc, q, k, v):
+    """One stream: out, lse, q [n_new][heads][.], k, v [n_new][128]."""
+    n, group, _ = q.shape
+    got, gl = out.float().cpu().double().numpy(), lse.cpu().double().numpy()
+    q, k, v = (x.double().numpy() for x in (q, k, v))
+    ck, cv = oc.reconstruct(oc.streams[(0, 0, 0)])
+    kk, vv = np.concatenate([ck, k]), np.concatenate([cv, v])
+    hide = np.arange(len(kk))[None] > len(ck) + np.arange(n)[:, None]
+    seen = np.where(hide, 0.0, 1.0)
+    floor = 2.0 ** -32 * (seen @ np.abs(vv)) if n * group > 64 else 3.75 * 2.0 ** -36 * (seen @ np.abs(vv).max(1))[:, None]
+    num = den = lnum = lden = 0.0
+    for a in range(group):
+        x = np.where(hide, -np.inf, q[:, a] @ kk.T * oc.scale)
+        mag = np.where(hide, 0, np.abs(q[:, a]) @ np.abs(kk.T) * oc.scale).max(1)
+        top = x.max(1)
+        rl = top + np.log(np.exp(x - top[:, None]).sum(1))
+        w = np.exp(x - rl[:, None])
+        o, ov = w @ vv, w @ np.abs(vv)
+        slack = (2.0 ** -16 + 2.0 ** -21) * mag + 2.0 ** -20
+        tol = (2 * slack[:, None] + 2.0 ** -8 + 2.0 ** -11) * ov + 2.0 ** -8 * np.abs(o) + floor
+        err = np.abs(got[:, a] - o)
+        assert (err <= tol * 1.01).all(), f"head {a}: off by {np.nanmax(err - tol):.3e} more than the bound"
+        assert (np.abs(gl[:, a] - rl) <= slack + 2.0 ** -21 * np.abs(rl)).all(), f"head {a}: log-sum-exp off by {np.abs(gl[:, a] - rl).max():.3e}"
+        num, den = num + (np.maximum(err - floor, 0) ** 2).sum(), den + (o ** 2).sum()
+        lnum, lden = lnum + ((gl[:, a] - rl) ** 2).sum(), lden + (rl ** 2).sum()
+    assert num <= (4e-3) ** 2 * den, f"off by {math.sqrt(num / den):.2e} of the norm"
+    assert lnum <= (4e-6) ** 2 * lden, f"log-sum-exp off by {math.sqrt(lnum / lden):.2e} of its norm"
 
 
 def run_alike(c, oc, q, k, v, batch, n_kv):
@@ -44,7 +80,7 @@ def run_alike(c, oc, q, k, v, batch, n_kv):
             key = o.float().cpu().numpy().tobytes() + l.cpu().numpy().tobytes()
             if key not in seen:
                 seen[key] = True
-                check(o[None], l[None], oc, q[None], k[None], v[None])
+                check(o, l, oc, q, k[:, 0], v[:, 0])
     return out, lse
 
 
@@ -147,3 +183,18 @@ def test_a_leading_key_and_many_rows(level, lead, noise):
     k, v, x = sink(ctx, 40, 4, lead, 1.0, noise, seed=level)
     c, oc = streams_alike(k, v, plan(ctx, level), 1, 2, 4)
     run_alike(c, oc, *x, 1, 2)
+
+
+@pytest.mark.parametrize("level", [8, 4, 2])
+@pytest.mark.parametrize("lead", [13.7, 40.0])
+@pytest.mark.parametrize("n_new", [6, 40])
+def test_a_large_logit_over_codes(level, lead, n_new):
+    """One channel makes the largest logit, of a key that is stored as codes and whose value counts."""
+    ctx, at = 64 * 23 + 3, 272
+    g = torch.Generator().manual_seed(level)
+    q, k, v = 0.1 * torch.randn(n_new, 4, 128, generator=g), torch.randn(ctx + n_new, 128, generator=g), torch.randn(ctx + n_new, 128, generator=g)
+    q[..., 0], k[:, 0], k[at] = 8.0, 0.0, 0.0
+    k[at, 0] = lead * math.sqrt(128.0) / 8.0
+    q, k, v = q.bfloat16(), k.bfloat16(), v.bfloat16()
+    c, oc = streams_alike(k[:ctx], v[:ctx], plan(ctx, level, first=level), 1, 2, 4)
+    run_alike(c, oc, q, k[ctx:, None], v[ctx:, None], 1, 2)
