@@ -184,9 +184,13 @@ GKV_API int gkv_decode_attn_observe(gkv_cache* c, int32_t layer, const void* q, 
  *   k_new, v_new  device bf16 [batch][n_new][n_kv_heads][128], 16-byte aligned (values of real tokens finite)
  *   len    HOST int32 [batch], 0 .. n_new: real tokens of each sequence (the rest of its rows is neither read for a result nor
  *          written), read during the call only; or NULL = n_new everywhere.  At most 1024 sequences with lengths (GKV_ERR_UNSUPPORTED)
- *          (values within +-65504, the cache's exact rows too: rows become fp16 where there are many; larger ones are clamped there)
+ *          (rows within +-65504, the cache's exact ones too: where there are many query rows (see gkv_chunk_workspace_bytes) all become fp16,
+ *          larger ones are clamped there, and queries, keys and values are multiples of 2^-24)
  *   out    device bf16 [batch][n_new][n_q_heads][128], 16-byte aligned: rounded once from fp32 accumulators.  Weights enter the value product with
- *          8 bits or more, values with 11; keys and logits keep 22
+ *          8 bits or more and values with 11.  A weight below 2^-24 of the row's heaviest is off by 2^-32 of that where there are many rows;
+ *          where there are few, one over codes below 2^-28 of the heaviest of its 32 keys by 2^-36 of that.  Logits of exact rows have their 32
+ *          bits but for what the tensor cores cut of a sum (2^-21 of scale * sum |q k| and less); over codes scale * sum |q| (s code + |z|)
+ *          takes the place of that, and they are off by up to 2^-19 of it where there are few rows
  *   lse    device fp32 [batch][n_new][n_q_heads], natural-log sum of exp(logit), or NULL
  *   workspace  device, 16-byte aligned, gkv_chunk_workspace_bytes long: partial results of the call, free again when its kernels
  *          are done.  Calls that may run at the same time need workspaces of their own (two captured graphs too); the launches of calls of

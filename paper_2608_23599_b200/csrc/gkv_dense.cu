@@ -2,8 +2,9 @@
 //
 // order_kernel   puts a stream's blocks in the order of their rows: those with 64 rows, then the centroids, one row each; queries become fp16 rows
 // expand_kernel  writes keys and values as fp16 rows: a quantised key as a pair hi + lo (22 bits: the log-sum-exp of a short context would
-//                otherwise miss 32 bits by the rounding of a few heavy keys), a value rounded once (2^-12 of itself).  Exact rows and the chunk's own
-//                rows become fp16 too, exactly but for values below 2^-14 (their last bits, kept in lo for keys) and beyond +-65504 (clamped)
+//                otherwise miss 32 bits by the rounding of a few heavy keys), a value rounded once (off by 2^-11 of itself at most, 2^-25 below 2^-14).
+//                Exact rows and the chunk's own rows become fp16 too, exactly but for numbers below 2^-14 (off by up to 2^-25, lo included: 2^-24 is
+//                fp16's last step) and beyond +-65504 (clamped)
 // attend_kernel  (gkv_attend.cuh) with a second product Q K_lo where keys have one, a term per key where some are hidden or stand for many (log2 of
 //                how many), and the chunk's own rows causally
 //

@@ -6,7 +6,7 @@
 // exactly as gkv_decode.cu reads it: codes are used as they lie (a code in the mantissa of an fp16 with a zero exponent field is code 2^(p - 24)),
 // the scaled query is an fp16 pair hi + lo formed once per half block, and q . z starts the accumulators.  Values the same way with
 // the scales in the weights: O += (P s) code, and sum_j p_j z_j in four more accumulators, one per group of 32 channels.  A scaled query is off by 2^-22 of
-// itself or 2^-25.  Weights are single numbers, as the bf16 output allows: bf16 (off by 2^-8 at most) over exact rows, relative to the row's reference; fp16
+// itself or 2^-25, a logit by what the tensor cores keep of products with codes (see code_exp): 2^-20 of a large one at 8 bits.  Weights are single numbers, as the bf16 output allows: bf16 (off by 2^-8 at most) over exact rows, relative to the row's reference; fp16
 // (2^-11) over codes, relative to the item's own maximum (weigh_codes, code_values), since fp16 has no room for those of a row whose keys lie far apart.
 //
 // What bounds it: at 4 bits a block of 64 tokens is 10 KB, 420 cycles of an SM's share of the copy bandwidth; its products are 212 MMAs per 16 rows,

@@ -113,7 +113,7 @@ def plan(ctx, level, first=16):
 @pytest.mark.parametrize("lead,noise", [(11.0, 0.3), (13.0, 0.0), (16.0, 0.0)])
 def test_a_leading_key_and_few_rows(level, gain, lead, noise):
     """More streams than CTAs, 64 rows: the team that meets the leading key reads a third of the context."""
-    ctx, batch, n_kv = 64 * 48, 20, 8
+    ctx, batch, n_kv = 64 * 50, 20, 8
     k, v, x = sink(ctx, 16, 4, lead, gain, noise, seed=level)
     c, oc = streams_alike(k, v, plan(ctx, level), batch, n_kv, 4)
     run_alike(c, oc, *x, batch, n_kv)
