@@ -184,8 +184,8 @@ inline int chunk_walk(int n) {
 }
 
 // ---- chunks of few rows (gkv_verify.cu): a tile is a stream, an item half a block, 32 keys ----
-// Rows up to which a chunk counts as one of few.  64 rows here and 68 and 96 written out: 16 streams of 8,200 tokens 41, 69 and 62 us, 64 of 16,384 tokens
-// 189, 339 and 325, two of 1,000 tokens 23, 29 and 32.  (Two tiles of up to 64 rows each would read the codes twice: 65 for 69, 255 for 339, but 82 for
+// Rows up to which a chunk counts as one of few.  64 rows here and 68 and 96 written out: 16 streams of 8,200 tokens 43, 68 and 62 us, 64 of 16,384 tokens
+// 206, 339 and 324, two of 1,000 tokens 21, 32 and 24.  (Two tiles of up to 64 rows each would read the codes twice: 65 for 69, 255 for 339, but 82 for
 // 64 and 378 for 327 at 128 rows.)
 constexpr int kVerifyRows = 64;
 inline void verify_shape(ChunkShape* s, int n_closed, int n_tail, int res_rows) {
